@@ -73,7 +73,9 @@ typedef enum {
     OCTNCA_ESPACE = -5        /* workspace too small */
 } octnca_status;
 
-typedef enum { OCTNCA_F32 = 0, OCTNCA_F16 = 1 } octnca_dtype;
+/* States and images are fp32 or fp16; bf16 is for gradient tensors only
+ * (octnca_param). */
+typedef enum { OCTNCA_F32 = 0, OCTNCA_F16 = 1, OCTNCA_BF16 = 2 } octnca_dtype;
 
 /* MLP arithmetic of the step kernel (octnca_model.mlp).  The step's
  * definition (Sec. 3.1) fixes no precision; these are the operand types the
@@ -419,6 +421,146 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
                           float fire_rate, uint64_t seed, const float *target, void *workspace,
                           size_t workspace_bytes, const octnca_level_grads *grads, double *loss,
                           void *final_state, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * State cache: states held in 8 bits.  A training pass keeps every state of
+ * every step for its backward; a cache holds them (or a pool of states, or the
+ * states of a long video) in about a quarter of the memory of fp32.
+ *
+ * A cache has `slots` states of `cells` cells.  Within a slot, block j is the
+ * cells j*block .. j*block + block - 1 in storage order (the last block may
+ * have fewer), and each channel of a block has one scale:
+ *   A = max of the block's |x| over its finite values of the channel,
+ *   a = max(A, 2^-100);
+ *   OCTNCA_CODE_I8: r = 127 / a, scale = a / 127 (both rounded to fp32),
+ *     code = x * r rounded to the nearest integer (ties to even), -127 .. 127;
+ *     -128 stands for a value that is not finite;
+ *   OCTNCA_CODE_F8: scale = the smallest power of two with a / scale <= 448,
+ *     code = x / scale rounded to the nearest fp8 e4m3 value (ties to even);
+ *     its NaN stands for a value that is not finite.
+ * Reading gives code * scale, computed in fp32 and rounded to the state's
+ * storage type; a value that was not finite reads back as NaN and leaves the
+ * others of its block as they are.
+ * ------------------------------------------------------------------------- */
+typedef enum { OCTNCA_CODE_I8 = 0, OCTNCA_CODE_F8 = 1 } octnca_code;
+
+typedef struct {
+    int32_t code;   /* octnca_code */
+    int32_t block;  /* cells that share a scale: 32, 64 or 128 */
+    int64_t slots;  /* states the cache has room for, >= 0 */
+    int64_t cells;  /* cells of one state, >= 1 */
+    void *codes;    /* [slots][cells][C], one byte each; 4-byte aligned */
+    float *scales;  /* [slots][ceil(cells / block)][C]; 16-byte aligned */
+} octnca_state_cache;
+
+/* Quantises cells from .. from + count - 1 of n states into their slots:
+ *   states  [n][count][C], the model's storage type, aligned to four values;
+ *   slots   device array [n], the slot of each state, or NULL: state i goes to
+ *           slot first + i.  An entry outside 0 .. slots - 1 is not written;
+ *           of equal entries the last one's state is kept.
+ * from is a multiple of block, and count too unless from + count = cells (a
+ * long state may be written piece by piece).  n = 0 or count = 0 writes
+ * nothing.  states must not overlap the cache.
+ * Errors: EINVAL, ESHAPE (a range outside the state or the cache), EUNSUPPORTED,
+ * EHIP. */
+int octree_nca_state_cache_write(const octnca_model *model, const octnca_state_cache *cache,
+                                 const void *states, int64_t from, int64_t count, int32_t n,
+                                 const int64_t *slots, int64_t first, void *stream);
+
+/* The values of cells from .. from + count - 1 of n slots, states [n][count][C].
+ * Arguments as for octree_nca_state_cache_write, but count is any number up to
+ * the end of the state, equal entries of `slots` all get their slot, and an
+ * entry outside 0 .. slots - 1 reads as zeros. */
+int octree_nca_state_cache_read(const octnca_model *model, const octnca_state_cache *cache,
+                                void *states, int64_t from, int64_t count, int32_t n,
+                                const int64_t *slots, int64_t first, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Gradients of many tensors: their global norm, clipping by it, and the
+ * clipped AdamW update (the paper trains with Adam and a running average of
+ * the weights, supplement S7).
+ *
+ * The tensors are listed once: octree_nca_param_table writes a table of them
+ * into caller-owned device memory, which the calls below read.  The table
+ * holds the tensors' addresses, not their values: it stays good while the
+ * tensors stay where they are.  It also holds the scratch memory of a call, so
+ * calls on one table must not overlap.
+ * ------------------------------------------------------------------------- */
+
+/* One tensor of a list.  Arrays are contiguous device memory, aligned to their
+ * element; count = 0 leaves the tensor out.  Over the list, `clipped`, `ema`
+ * and the three of param, m, v are either given for every tensor or for none
+ * (ema only with param).  Arrays must not overlap, except that clipped may be
+ * grad itself with the same type. */
+typedef struct {
+    int64_t count;        /* elements */
+    const void *grad;     /* [count] of grad_dtype */
+    void *clipped;        /* [count] of clipped_dtype: output of octree_nca_clip_grads; or NULL */
+    float *param, *m, *v; /* [count]: weights and moments of octree_nca_adamw; or NULL */
+    float *ema;           /* [count]: running average of the weights; or NULL */
+    int32_t grad_dtype;   /* octnca_dtype */
+    int32_t clipped_dtype;
+} octnca_param;
+
+/* A list whose table is written (host; filled by octree_nca_param_table). */
+typedef struct {
+    void *table;
+    int64_t chunks;
+    int64_t elements;
+    int32_t has;          /* bit 0 clipped, bit 1 param / m / v, bit 2 ema */
+} octnca_param_list;
+
+/* Bytes of table that a list needs (0 if the list is invalid). */
+size_t octree_nca_param_table_bytes(const octnca_param *params, int32_t n);
+
+/* Writes the table of `n` tensors (host array, read during the call) to
+ * `table` (16-byte aligned) and fills *list.  Errors: EINVAL (null or
+ * misaligned pointers, arrays given for some tensors only, overlaps, types),
+ * ESHAPE (count < 0 or too many elements), ESPACE, EHIP. */
+int octree_nca_param_table(const octnca_param *params, int32_t n, void *table, size_t table_bytes,
+                           octnca_param_list *list, void *stream);
+
+/* *norm (device) = scale * sqrt(sum over all gradients of g^2), summed in fp64.
+ * scale > 0 and finite (the inverse of a loss scale, or of a batch's size).
+ * The norm of no elements is 0.  Errors: EINVAL, EHIP. */
+int octree_nca_grad_norm(const octnca_param_list *list, float scale, float *norm, void *stream);
+
+/* clipped = grad * f with f = scale if norm <= max_norm, else scale * max_norm /
+ * norm, for the norm of octree_nca_grad_norm: f is rounded to fp32 once, the
+ * product once to clipped's type.  A gradient that is not finite shows: with an
+ * infinite norm the infinite ones become NaN and the others 0, with a NaN norm
+ * all become NaN (max_norm finite).
+ *   max_norm  > 0, may be infinite (no clipping);
+ *   norm      device fp32 or NULL: receives the norm.
+ * Errors: EINVAL (also a list without `clipped`), EHIP. */
+int octree_nca_clip_grads(const octnca_param_list *list, float scale, float max_norm, float *norm,
+                          void *stream);
+
+/* Settings of one AdamW update (decoupled weight decay). */
+typedef struct {
+    double lr;            /* >= 0 */
+    double beta1, beta2;  /* in [0, 1) */
+    double eps;           /* > 0 */
+    double weight_decay;  /* >= 0 */
+    double max_norm;      /* > 0, may be infinite: gradients are clipped to this global norm */
+    double scale;         /* > 0, finite: factor of the gradients before that */
+    double ema_decay;     /* in [0, 1]: weight of the old running average */
+} octnca_adamw;
+
+/* One update of all tensors of a list with param, m and v.  With f of
+ * octree_nca_clip_grads and t = *step + 1, in fp32:
+ *   g' = g f;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *   param -= lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *                + weight_decay param);
+ *   ema = ema_decay ema + (1 - ema_decay) param   (lists with ema);
+ *   *step = t.
+ * Where the norm is not finite nothing of this is written (*norm still is), as
+ * a step with an overflowed gradient is left out.
+ *   step  device int64: updates made so far, >= 0;
+ *   norm  device fp32 or NULL: receives the norm before clipping.
+ * The gradients are not changed.  Errors: EINVAL, EHIP. */
+int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings, int64_t *step,
+                     float *norm, void *stream);
 
 /* Static text for a status code; never NULL. */
 const char *octree_nca_strerror(int status);

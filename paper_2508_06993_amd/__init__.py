@@ -29,14 +29,20 @@ __all__ = [
     "octree_nca_step_backward_workspace_bytes", "octree_nca_step_backward",
     "octree_nca_upsample_backward", "octree_nca_readout_mse_workspace_bytes",
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
-    "level_grads_struct", "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
+    "level_grads_struct", "StateCacheBuffers", "octree_nca_state_cache_write",
+    "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
+    "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
+    "octree_nca_adamw", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
+    "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
     "OCTNCA_EUNSUPPORTED", "OCTNCA_ESHAPE",
     "OCTNCA_EHIP", "OCTNCA_ESPACE", "OCTNCA_F32", "OCTNCA_F16", "KERNEL_NAMES", "kernel_fields",
 ]
 
 OCTNCA_OK, OCTNCA_EINVAL, OCTNCA_EUNSUPPORTED, OCTNCA_ESHAPE, OCTNCA_EHIP, OCTNCA_ESPACE = \
     0, -1, -2, -3, -4, -5
-OCTNCA_F32, OCTNCA_F16 = 0, 1
+OCTNCA_F32, OCTNCA_F16, OCTNCA_BF16 = 0, 1, 2
+OCTNCA_CODE_I8, OCTNCA_CODE_F8 = 0, 1
+CODE_NAMES = {"i8": OCTNCA_CODE_I8, "f8": OCTNCA_CODE_F8}   # formats of a state cache
 (OCTNCA_MLP_AUTO, OCTNCA_MLP_F32, OCTNCA_MLP_BF16X3, OCTNCA_MLP_F16, OCTNCA_MLP_F16S,
  OCTNCA_MLP_VALU) = range(6)
 OCTNCA_LAYOUT_AUTO, OCTNCA_LAYOUT_ROWS, OCTNCA_LAYOUT_TILES = range(3)
@@ -77,6 +83,9 @@ EXPORTED_SYMBOLS = (
     "octree_nca_step_backward_workspace_bytes", "octree_nca_step_backward",
     "octree_nca_upsample_backward", "octree_nca_readout_mse_workspace_bytes",
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
+    "octree_nca_state_cache_write", "octree_nca_state_cache_read",
+    "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm",
+    "octree_nca_clip_grads", "octree_nca_adamw",
 )
 
 
@@ -107,8 +116,32 @@ class _LevelGrads(ctypes.Structure):
                 ("w1", ctypes.c_void_p), ("b1", ctypes.c_void_p), ("w2", ctypes.c_void_p)]
 
 
+class _StateCache(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_int32), ("block", ctypes.c_int32), ("slots", ctypes.c_int64),
+                ("cells", ctypes.c_int64), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
+
+
+class _Param(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("grad", ctypes.c_void_p),
+                ("clipped", ctypes.c_void_p), ("param", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("ema", ctypes.c_void_p), ("grad_dtype", ctypes.c_int32),
+                ("clipped_dtype", ctypes.c_int32)]
+
+
+class _ParamList(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64),
+                ("elements", ctypes.c_int64), ("has", ctypes.c_int32)]
+
+
+class _AdamW(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_double) for k in
+                ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm", "scale", "ema_decay")]
+
+
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
 _SIGS = {
     "octree_nca_build_pyramid": (_I32, [ctypes.POINTER(_Model), _P, _Extent, _I32,
                                         ctypes.POINTER(_I32), ctypes.POINTER(_P), _P]),
@@ -158,6 +191,17 @@ _SIGS = {
                                      ctypes.POINTER(_I32), ctypes.c_float, ctypes.c_uint64, _P,
                                      _P, ctypes.c_size_t, ctypes.POINTER(_LevelGrads), _P, _P,
                                      _P]),
+    "octree_nca_state_cache_write": (_I32, [ctypes.POINTER(_Model), ctypes.POINTER(_StateCache),
+                                            _P, _I64, _I64, _I32, _P, _I64, _P]),
+    "octree_nca_state_cache_read": (_I32, [ctypes.POINTER(_Model), ctypes.POINTER(_StateCache),
+                                           _P, _I64, _I64, _I32, _P, _I64, _P]),
+    "octree_nca_param_table_bytes": (ctypes.c_size_t, [ctypes.POINTER(_Param), _I32]),
+    "octree_nca_param_table": (_I32, [ctypes.POINTER(_Param), _I32, _P, ctypes.c_size_t,
+                                      ctypes.POINTER(_ParamList), _P]),
+    "octree_nca_grad_norm": (_I32, [ctypes.POINTER(_ParamList), ctypes.c_float, _P, _P]),
+    "octree_nca_clip_grads": (_I32, [ctypes.POINTER(_ParamList), ctypes.c_float, ctypes.c_float,
+                                     _P, _P]),
+    "octree_nca_adamw": (_I32, [ctypes.POINTER(_ParamList), ctypes.POINTER(_AdamW), _P, _P, _P]),
     "octree_nca_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "octree_nca_abi_version": (ctypes.c_int, []),
 }
@@ -511,3 +555,146 @@ def octree_nca_train_step(model: Model, image, factors, weights, steps, fire_rat
         workspace.numel() * workspace.element_size(), gs, _ptr(loss, torch.float64, "loss"),
         _ptr(final_state, torch.float32, "final_state"), _stream(stream))
     _check(st, "octree_nca_train_step")
+
+
+# ---------------------------------------------------------------------------
+# state cache: states in 8 bits
+# ---------------------------------------------------------------------------
+
+@dataclass
+class StateCacheBuffers:
+    """A cache's description and device memory (octnca_state_cache): codes int8
+    or uint8 [slots][cells][C], scales fp32 [slots][ceil(cells / block)][C]."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cells: int
+    code: str = "i8"
+    block: int = 64
+
+    def struct(self, model: Model) -> _StateCache:
+        if self.code not in CODE_NAMES:
+            raise ValueError(f"unknown code {self.code!r}; known: {sorted(CODE_NAMES)}")
+        if self.block not in (32, 64, 128):
+            raise ValueError(f"block is 32, 64 or 128 cells, got {self.block}")
+        if self.codes.dtype not in (torch.int8, torch.uint8):
+            raise OctreeNCAError(f"codes: expected int8 or uint8, got {self.codes.dtype}")
+        slots, c = self.codes.shape[0], model.channels
+        if tuple(self.codes.shape) != (slots, self.cells, c):
+            raise OctreeNCAError(f"codes: expected shape {(slots, self.cells, c)}, "
+                                 f"got {tuple(self.codes.shape)}")
+        want = (slots, -(-self.cells // self.block), c)
+        if tuple(self.scales.shape) != want:
+            raise OctreeNCAError(f"scales: expected shape {want}, got {tuple(self.scales.shape)}")
+        return _StateCache(CODE_NAMES[self.code], self.block, slots, self.cells,
+                           _ptr(self.codes, None, "codes"),
+                           _ptr(self.scales, torch.float32, "scales"))
+
+
+def _cache_call(name, model, cache, states, from_cell, slots, first, stream):
+    """states: [n][cells...][C]; n = the slots named by ``slots`` (int64 tensor),
+    or the states' first axis."""
+    n, c = states.shape[0], states.shape[-1]
+    if c != model.channels:
+        raise OctreeNCAError(f"states: expected {model.channels} channels, got {c}")
+    if slots is not None and tuple(slots.shape) != (n,):
+        raise OctreeNCAError(f"slots: expected shape {(n,)}, got {tuple(slots.shape)}")
+    count = 1
+    for v in states.shape[1:-1]:
+        count *= v
+    st = getattr(lib(), name)(ctypes.byref(model.struct()), ctypes.byref(cache.struct(model)),
+                              _ptr(states, model.torch_dtype, "states"), int(from_cell), count, n,
+                              _ptr(slots, torch.int64, "slots"), int(first), _stream(stream))
+    _check(st, name)
+
+
+def octree_nca_state_cache_write(model: Model, cache: StateCacheBuffers, states, from_cell=0,
+                                 slots=None, first=0, stream=None) -> None:
+    """Quantise states [n][...cells][C] into the slots ``slots`` (device int64
+    [n]) or first, first + 1, ..."""
+    _cache_call("octree_nca_state_cache_write", model, cache, states, from_cell, slots, first,
+                stream)
+
+
+def octree_nca_state_cache_read(model: Model, cache: StateCacheBuffers, states, from_cell=0,
+                                slots=None, first=0, stream=None) -> None:
+    """Fill states [n][...cells][C] with the values of the slots."""
+    _cache_call("octree_nca_state_cache_read", model, cache, states, from_cell, slots, first,
+                stream)
+
+
+# ---------------------------------------------------------------------------
+# gradients of many tensors
+# ---------------------------------------------------------------------------
+
+_GRAD_TYPES = {torch.float32: OCTNCA_F32, torch.float16: OCTNCA_F16, torch.bfloat16: OCTNCA_BF16}
+
+
+def _grad_type(t, name):
+    if t.dtype not in _GRAD_TYPES:
+        raise OctreeNCAError(f"{name}: expected fp32, fp16 or bf16, got {t.dtype}")
+    return _GRAD_TYPES[t.dtype]
+
+
+def param_structs(grads, params=None, m=None, v=None, ema=None, clipped=None):
+    """Array of octnca_param for lists of device tensors (index = tensor)."""
+    n = len(grads)
+    lists = {"clipped": clipped, "param": params, "m": m, "v": v, "ema": ema}
+    for k, x in lists.items():
+        if x is not None and len(x) != n:
+            raise OctreeNCAError(f"{k}: {len(x)} tensors for {n} gradients")
+    out = (_Param * max(1, n))()
+    for i, g in enumerate(grads):
+        p = out[i]
+        p.count, p.grad, p.grad_dtype = g.numel(), _ptr(g, None, "grad"), _grad_type(g, "grad")
+        for k, x in lists.items():
+            if x is None:
+                continue
+            if x[i].numel() != p.count:
+                raise OctreeNCAError(f"{k}: {x[i].numel()} elements for {p.count} of the gradient")
+            if x[i].device != g.device:
+                raise OctreeNCAError(f"{k}: on {x[i].device}, the gradient on {g.device}")
+            setattr(p, k, _ptr(x[i], None if k == "clipped" else torch.float32, k))
+        if clipped is not None:
+            p.clipped_dtype = _grad_type(clipped[i], "clipped")
+    return out
+
+
+def octree_nca_param_table_bytes(structs, n: int) -> int:
+    size = int(lib().octree_nca_param_table_bytes(structs, n))
+    if size == 0:
+        raise OctreeNCAError("octree_nca_param_table_bytes: invalid list", OCTNCA_EINVAL)
+    return size
+
+
+def octree_nca_param_table(structs, n: int, table, stream=None) -> _ParamList:
+    """Writes the table of a list (param_structs) to the uint8 tensor ``table``."""
+    out = _ParamList()
+    st = lib().octree_nca_param_table(structs, n, _ptr(table, torch.uint8, "table"),
+                                      table.numel(), ctypes.byref(out), _stream(stream))
+    _check(st, "octree_nca_param_table")
+    return out
+
+
+def octree_nca_grad_norm(plist: _ParamList, norm, scale=1.0, stream=None) -> None:
+    """norm: device fp32 tensor of one element."""
+    st = lib().octree_nca_grad_norm(ctypes.byref(plist), float(scale),
+                                    _ptr(norm, torch.float32, "norm"), _stream(stream))
+    _check(st, "octree_nca_grad_norm")
+
+
+def octree_nca_clip_grads(plist: _ParamList, max_norm: float, scale=1.0, norm=None,
+                          stream=None) -> None:
+    st = lib().octree_nca_clip_grads(ctypes.byref(plist), float(scale), float(max_norm),
+                                     _ptr(norm, torch.float32, "norm"), _stream(stream))
+    _check(st, "octree_nca_clip_grads")
+
+
+def octree_nca_adamw(plist: _ParamList, step, lr: float, betas=(0.9, 0.99), eps=1e-8,
+                     weight_decay=0.0, max_norm=float("inf"), scale=1.0, ema_decay=0.0, norm=None,
+                     stream=None) -> None:
+    """step: device int64 tensor of one element, the updates made so far."""
+    h = _AdamW(lr, betas[0], betas[1], eps, weight_decay, max_norm, scale, ema_decay)
+    st = lib().octree_nca_adamw(ctypes.byref(plist), ctypes.byref(h),
+                                _ptr(step, torch.int64, "step"),
+                                _ptr(norm, torch.float32, "norm"), _stream(stream))
+    _check(st, "octree_nca_adamw")

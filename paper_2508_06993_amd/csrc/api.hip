@@ -10,7 +10,9 @@
 #include <cmath>
 #include <algorithm>
 #include <mutex>
+#include <new>
 #include <utility>
+#include <vector>
 #include "launch.h"
 #include "octree_nca.h"
 
@@ -1179,6 +1181,226 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
         }
     }
     return OCTNCA_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxCacheBytes = int64_t(1) << 60;
+
+// Checks a cache and a call's range; fills the kernels' arguments.
+int make_cache_args(const octnca_model *m, const octnca_state_cache *c, const void *states,
+                    int64_t from, int64_t count, int32_t n, const int64_t *slots, int64_t first,
+                    bool write, CacheArgs *a) {
+    const int st = check_model(m);
+    if (st) return st;
+    if (c == nullptr || n < 0 || from < 0 || count < 0) return OCTNCA_EINVAL;
+    if (c->code != OCTNCA_CODE_I8 && c->code != OCTNCA_CODE_F8) return OCTNCA_EINVAL;
+    if (c->block != 32 && c->block != 64 && c->block != 128) return OCTNCA_EINVAL;
+    if (c->slots < 0 || c->cells < 1 || c->cells > kMaxCells) return OCTNCA_ESHAPE;
+    const int64_t blocks = (c->cells + c->block - 1) / c->block;
+    const int64_t slot_bytes = c->cells * m->channels;            // <= 2^36 * 20
+    if (c->slots > kMaxCacheBytes / (slot_bytes + 4 * blocks * m->channels)) return OCTNCA_ESHAPE;
+    if (from % c->block != 0) return OCTNCA_EINVAL;
+    if (from > c->cells || count > c->cells - from) return OCTNCA_ESHAPE;
+    if (write && count % c->block != 0 && from + count != c->cells) return OCTNCA_EINVAL;
+    if (slots == nullptr && n > 0 && (first < 0 || first > c->slots || n > c->slots - first))
+        return OCTNCA_ESHAPE;
+    a->n = n;
+    a->count = count;
+    if (n == 0 || count == 0) return OCTNCA_OK;
+    const uintptr_t state_align = 4 * elem_bytes(m);
+    const bool no_cache = c->slots == 0;   // every entry of `slots` is outside
+    if (states == nullptr || (!no_cache && (c->codes == nullptr || c->scales == nullptr)) ||
+        (uintptr_t)states % state_align || (uintptr_t)c->codes % 4 || (uintptr_t)c->scales % 16 ||
+        (uintptr_t)slots % 8)
+        return OCTNCA_EINVAL;
+    if (count > kMaxCacheBytes / n / m->channels / 4) return OCTNCA_ESHAPE;
+    const size_t state_bytes = (size_t)(count * n) * m->channels * elem_bytes(m);
+    if (overlap(states, state_bytes, c->codes, (size_t)(slot_bytes * c->slots)) ||
+        overlap(states, state_bytes, c->scales, (size_t)(4 * blocks * m->channels * c->slots)) ||
+        (slots && overlap(states, state_bytes, slots, (size_t)n * 8)))
+        return OCTNCA_EINVAL;
+    a->codes = (int8_t *)c->codes;
+    a->scales = c->scales;
+    a->n_slots = c->slots;
+    a->cells = c->cells;
+    a->blocks = blocks;
+    a->from = from;
+    a->slots = slots;
+    a->first = first;
+    a->block = c->block;
+    a->channels = m->channels;
+    a->f8 = c->code == OCTNCA_CODE_F8;
+    return OCTNCA_OK;
+}
+
+// A contiguous array of a parameter list, for the overlap check.
+struct Range {
+    uintptr_t begin, end;
+    bool written;
+};
+
+size_t dtype_bytes(int32_t t) { return t == OCTNCA_F32 ? 4 : 2; }
+bool grad_type(int32_t t) { return t == OCTNCA_F32 || t == OCTNCA_F16 || t == OCTNCA_BF16; }
+bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
+
+// Chunks, elements and arrays of a list (octnca_param_list without its table).
+int check_params(const octnca_param *params, int32_t n, octnca_param_list *l) {
+    if (n < 0 || (n > 0 && params == nullptr)) return OCTNCA_EINVAL;
+    l->table = nullptr;
+    l->chunks = l->elements = 0;
+    l->has = 0;
+    bool any = false;
+    for (int32_t i = 0; i < n; ++i) {
+        const octnca_param &t = params[i];
+        if (t.count < 0 || t.count > kMaxCells) return OCTNCA_ESHAPE;
+        if (t.count == 0) continue;
+        if (t.grad == nullptr || !grad_type(t.grad_dtype) ||
+            misaligned(t.grad, dtype_bytes(t.grad_dtype)))
+            return OCTNCA_EINVAL;
+        if (t.clipped && (!grad_type(t.clipped_dtype) ||
+                          misaligned(t.clipped, dtype_bytes(t.clipped_dtype))))
+            return OCTNCA_EINVAL;
+        const int given = (t.param != nullptr) + (t.m != nullptr) + (t.v != nullptr);
+        if ((given != 0 && given != 3) || (t.ema && given == 0)) return OCTNCA_EINVAL;
+        if (misaligned(t.param, 4) || misaligned(t.m, 4) || misaligned(t.v, 4) ||
+            misaligned(t.ema, 4))
+            return OCTNCA_EINVAL;
+        const int32_t has = (t.clipped ? kHasClipped : 0) | (t.param ? kHasParam : 0) |
+                            (t.ema ? kHasEma : 0);
+        if (any && has != l->has) return OCTNCA_EINVAL;
+        any = true;
+        l->has = has;
+        l->elements += t.count;
+        l->chunks += (t.count + kParamChunk - 1) / kParamChunk;
+        if (l->elements > kMaxCells) return OCTNCA_ESHAPE;
+    }
+    return OCTNCA_OK;
+}
+
+// Whether an array that a call writes overlaps another one of the list.
+bool params_overlap(const octnca_param *params, int32_t n) {
+    std::vector<Range> r;
+    r.reserve((size_t)n * 6);
+    for (int32_t i = 0; i < n; ++i) {
+        const octnca_param &t = params[i];
+        if (t.count == 0) continue;
+        auto add = [&](const void *p, size_t bytes, bool written) {
+            if (p) r.push_back({(uintptr_t)p, (uintptr_t)p + bytes * (size_t)t.count, written});
+        };
+        const bool in_place = t.clipped == t.grad && t.clipped_dtype == t.grad_dtype;
+        add(t.grad, dtype_bytes(t.grad_dtype), in_place);
+        if (!in_place) add(t.clipped, dtype_bytes(t.clipped_dtype), true);
+        add(t.param, 4, true);
+        add(t.m, 4, true);
+        add(t.v, 4, true);
+        add(t.ema, 4, true);
+    }
+    std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    uintptr_t read_end = 0, write_end = 0;   // of the ranges so far
+    for (const Range &x : r) {
+        if (x.begin < write_end || (x.written && x.begin < read_end)) return true;
+        (x.written ? write_end : read_end) = std::max(x.written ? write_end : read_end, x.end);
+    }
+    return false;
+}
+
+bool list_ok(const octnca_param_list *l, int32_t need) {
+    if (l == nullptr || l->table == nullptr || l->chunks < 0) return false;
+    return l->chunks == 0 || (l->has & need) == need;
+}
+
+bool positive(double x) { return x > 0.0 && x < HUGE_VAL; }
+
+}  // namespace
+
+extern "C" {
+
+int octree_nca_state_cache_write(const octnca_model *model, const octnca_state_cache *cache,
+                                 const void *states, int64_t from, int64_t count, int32_t n,
+                                 const int64_t *slots, int64_t first, void *stream) {
+    CacheArgs a{};
+    const int st = make_cache_args(model, cache, states, from, count, n, slots, first, true, &a);
+    if (st || n == 0 || count == 0) return st;
+    return hip_status(launch_cache_write((Dtype)model->state_dtype, a, states,
+                                         (hipStream_t)stream));
+}
+
+int octree_nca_state_cache_read(const octnca_model *model, const octnca_state_cache *cache,
+                                void *states, int64_t from, int64_t count, int32_t n,
+                                const int64_t *slots, int64_t first, void *stream) {
+    CacheArgs a{};
+    const int st = make_cache_args(model, cache, states, from, count, n, slots, first, false, &a);
+    if (st || n == 0 || count == 0) return st;
+    return hip_status(launch_cache_read((Dtype)model->state_dtype, a, states,
+                                        (hipStream_t)stream));
+}
+
+size_t octree_nca_param_table_bytes(const octnca_param *params, int32_t n) {
+    octnca_param_list l;
+    return check_params(params, n, &l) ? 0 : param_table_bytes(l.chunks);
+}
+
+int octree_nca_param_table(const octnca_param *params, int32_t n, void *table, size_t table_bytes,
+                           octnca_param_list *list, void *stream) {
+    octnca_param_list l;
+    const int st = check_params(params, n, &l);
+    if (st) return st;
+    if (table == nullptr || list == nullptr || misaligned(table, 16)) return OCTNCA_EINVAL;
+    try {   // the check's own list may run out of memory
+        if (params_overlap(params, n)) return OCTNCA_EINVAL;
+    } catch (const std::bad_alloc &) {
+        return OCTNCA_ESPACE;
+    }
+    const size_t need = param_table_bytes(l.chunks);
+    if (table_bytes < need) return OCTNCA_ESPACE;
+    for (int32_t i = 0; i < n; ++i) {
+        const octnca_param &t = params[i];
+        const size_t c = (size_t)t.count;
+        if (c == 0) continue;
+        if (overlap(table, need, t.grad, c * dtype_bytes(t.grad_dtype)) ||
+            (t.clipped && overlap(table, need, t.clipped, c * dtype_bytes(t.clipped_dtype))) ||
+            (t.param && (overlap(table, need, t.param, c * 4) || overlap(table, need, t.m, c * 4) ||
+                         overlap(table, need, t.v, c * 4))) ||
+            (t.ema && overlap(table, need, t.ema, c * 4)))
+            return OCTNCA_EINVAL;
+    }
+    if (launch_param_table(params, n, table, (hipStream_t)stream) != hipSuccess)
+        return OCTNCA_EHIP;
+    l.table = table;
+    *list = l;
+    return OCTNCA_OK;
+}
+
+int octree_nca_grad_norm(const octnca_param_list *list, float scale, float *norm, void *stream) {
+    if (!list_ok(list, 0) || !positive(scale) || norm == nullptr || misaligned(norm, 4))
+        return OCTNCA_EINVAL;
+    return hip_status(launch_grad_norm(*list, scale, norm, (hipStream_t)stream));
+}
+
+int octree_nca_clip_grads(const octnca_param_list *list, float scale, float max_norm, float *norm,
+                          void *stream) {
+    if (!list_ok(list, kHasClipped) || !positive(scale) || !(max_norm > 0.0f) ||
+        misaligned(norm, 4))
+        return OCTNCA_EINVAL;
+    return hip_status(launch_clip_grads(*list, scale, max_norm, norm, (hipStream_t)stream));
+}
+
+int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings, int64_t *step,
+                     float *norm, void *stream) {
+    if (!list_ok(list, kHasParam) || settings == nullptr || step == nullptr ||
+        misaligned(step, 8) || misaligned(norm, 4))
+        return OCTNCA_EINVAL;
+    const octnca_adamw &h = *settings;
+    auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
+    auto not_negative = [](double x) { return x >= 0.0 && x < HUGE_VAL; };
+    if (!not_negative(h.lr) || !beta_ok(h.beta1) || !beta_ok(h.beta2) || !positive((float)h.eps) ||
+        !not_negative(h.weight_decay) || !(h.max_norm > 0.0) || !positive(h.scale) ||
+        !(h.ema_decay >= 0.0 && h.ema_decay <= 1.0))
+        return OCTNCA_EINVAL;
+    return hip_status(launch_adamw(*list, h, step, norm, (hipStream_t)stream));
 }
 
 }  // extern "C"

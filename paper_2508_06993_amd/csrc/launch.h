@@ -9,6 +9,7 @@
 #include <atomic>
 
 #include "device_common.h"
+#include "octree_nca.h"
 
 namespace octnca {
 
@@ -205,6 +206,37 @@ hipError_t launch_step2_mfma_up(const StepArgs &a, MfmaMlp mlp, Layout2d layout,
 hipError_t launch_step_mfma_up(const StepArgs &a, Layout2d layout, const void *coarse,
                                int coarse_h, int coarse_w, int fz, int fy, int fx,
                                const void *img, void *dst, hipStream_t stream);
+
+// State cache (state_cache.hip): cells from .. from + count - 1 of n states to
+// and from their slots.  states: [n][count][channels] of dt.
+struct CacheArgs {
+    int8_t *codes;          // [n_slots][cells][channels]
+    float *scales;          // [n_slots][blocks][channels]
+    int64_t n_slots, cells, blocks;   // blocks: of a slot
+    int64_t from, count;
+    const int64_t *slots;   // device [n] or null: slot first + i
+    int64_t first;
+    int n, block, channels;
+    bool f8;
+};
+hipError_t launch_cache_write(Dtype dt, const CacheArgs &a, const void *states,
+                              hipStream_t stream);
+hipError_t launch_cache_read(Dtype dt, const CacheArgs &a, void *states, hipStream_t stream);
+
+// Tables of parameter tensors (params.hip).  A table is the scratch memory of a
+// call followed by the chunks: pieces of at most kParamChunk elements of one
+// tensor.  param_has_*: which arrays the list's tensors have.
+constexpr int kParamChunk = 4096;
+enum : int32_t { kHasClipped = 1, kHasParam = 2, kHasEma = 4 };
+size_t param_table_bytes(int64_t chunks);
+hipError_t launch_param_table(const octnca_param *params, int n, void *table, hipStream_t stream);
+// Sum of squares of all gradients (table scratch), then what it is for.
+hipError_t launch_grad_norm(const octnca_param_list &l, double scale, float *norm,
+                            hipStream_t stream);
+hipError_t launch_clip_grads(const octnca_param_list &l, double scale, double max_norm,
+                             float *norm, hipStream_t stream);
+hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64_t *step,
+                        float *norm, hipStream_t stream);
 
 // Compute units of the current device, cached per device.  Host threads may
 // call this concurrently: racing first calls store the same value.

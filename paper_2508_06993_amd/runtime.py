@@ -10,7 +10,10 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import Model, octree_nca_infer, octree_nca_workspace_bytes
+from . import (Model, StateCacheBuffers, octree_nca_adamw, octree_nca_clip_grads,
+               octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
+               octree_nca_param_table_bytes, octree_nca_state_cache_read,
+               octree_nca_state_cache_write, octree_nca_workspace_bytes, param_structs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
 
@@ -63,3 +66,81 @@ def infer(model: Model, image: torch.Tensor, factors, weights, steps, fire_rate:
     """One-shot inference; returns (final state, seg) as device tensors."""
     run = Inference(model, image.shape[:3], factors, device=image.device)
     return run(image, weights, steps, fire_rate, seed, stream=stream)
+
+
+class StateCache:
+    """States of one model and extent held in 8 bits (octnca_state_cache):
+    ``slots`` of them, each channel of ``block`` consecutive cells with one
+    scale.  ``codes`` / ``scales``: device memory to use instead of new."""
+
+    def __init__(self, model: Model, extent: Sequence[int], slots: int, code="i8", block=64,
+                 codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 device="cuda"):
+        self.model = model
+        self.extent = tuple(int(v) for v in extent)
+        d, h, w = self.extent
+        cells, c = d * h * w, model.channels
+        if codes is None:
+            codes = torch.zeros((slots, cells, c), dtype=torch.int8, device=device)
+        if scales is None:
+            scales = torch.zeros((slots, -(-cells // block), c), device=device)
+        self.buffers = StateCacheBuffers(codes, scales, cells, code, block)
+        self.buffers.struct(model)      # checks the description
+
+    def write(self, states: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0,
+              from_cell=0, stream=None) -> None:
+        """states [n][...][C]: whole states, or their cells from ``from_cell`` on.
+        ``slots``: device int64 [n], entries outside the cache are left out; or
+        None for slots first, first + 1, ..."""
+        octree_nca_state_cache_write(self.model, self.buffers, states, from_cell, slots, first,
+                                     stream)
+
+    def read(self, out: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0, from_cell=0,
+             stream=None) -> torch.Tensor:
+        """Fills and returns ``out`` [n][...][C]; slots outside the cache read as zeros."""
+        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first, stream)
+        return out
+
+
+class Parameters:
+    """Many tensors with their gradients, listed once: global norm, clipping and
+    the clipped AdamW update, a few launches whatever their number.
+
+    ``grads`` are fp32, fp16 or bf16; ``clipped`` (fp32, fp16 or bf16; may be
+    ``grads``) receives the clipped gradients; ``params``, ``m``, ``v`` and
+    ``ema`` are fp32.  The tensors are read and written where they are: the list
+    keeps them alive, and they must not be replaced by others.  ``step`` is the
+    number of updates made so far (device int64 [1]).  Calls of one list must
+    not overlap (it holds their scratch memory)."""
+
+    def __init__(self, grads, params=None, m=None, v=None, ema=None, clipped=None,
+                 step: Optional[torch.Tensor] = None, stream=None):
+        self.tensors = [list(x) if x is not None else None
+                        for x in (grads, params, m, v, ema, clipped)]
+        device = self.tensors[0][0].device if self.tensors[0] else torch.device("cuda")
+        structs = param_structs(*self.tensors)
+        n = len(self.tensors[0])
+        self.table = torch.empty(octree_nca_param_table_bytes(structs, n), dtype=torch.uint8,
+                                 device=device)
+        self.list = octree_nca_param_table(structs, n, self.table, stream)
+        self.norm = torch.zeros((), device=device)
+        self.step = step if step is not None else torch.zeros(1, dtype=torch.int64, device=device)
+
+    def grad_norm(self, scale=1.0, stream=None) -> torch.Tensor:
+        """scale * (2-norm of all gradients), a device scalar that the next call overwrites."""
+        octree_nca_grad_norm(self.list, self.norm, scale, stream)
+        return self.norm
+
+    def clip(self, max_norm: float, scale=1.0, stream=None) -> torch.Tensor:
+        """clipped = scale * gradients, shortened to ``max_norm`` if their norm
+        is larger; returns the norm (as grad_norm)."""
+        octree_nca_clip_grads(self.list, max_norm, scale, self.norm, stream)
+        return self.norm
+
+    def adamw(self, lr: float, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0,
+              max_norm=float("inf"), scale=1.0, ema_decay=0.99, stream=None) -> torch.Tensor:
+        """One update with the clipped gradients; left out if their norm is not
+        finite.  Returns the norm before clipping (as grad_norm)."""
+        octree_nca_adamw(self.list, self.step, lr, betas, eps, weight_decay, max_norm, scale,
+                         ema_decay, self.norm, stream)
+        return self.norm

@@ -1,0 +1,303 @@
+"""Gradient norm, clipping and the clipped AdamW update against their formulas
+in 64 bits.
+
+Bounds.  The norm is a 64-bit sum rounded to fp32: 2^-23 relative.  A clipped
+gradient is g f with f rounded to fp32 once (2^-24) and the product once (2^-24):
+2^-22 relative in fp32, with the half unit of fp16 (2^-11) or bf16 (2^-8) on top
+in those types.  The update is a few fp32 operations, each within 2^-24 of its
+terms' sizes; a bound per element is formed from them below."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_06993_amd as octnca
+from paper_2508_06993_amd.runtime import Parameters
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+LEAST = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}   # half the smallest value
+COUNTS = [1, 2, 3, 5, 0, 16, 64, 1000, 2048, 4095, 4096, 4097, 12289, 20001]
+LISTS = {"one": [1], "small": [7], "model": [144, 16, 2048, 64, 1024] * 5, "sizes": COUNTS,
+         "many": [1 + (37 * k) % 611 for k in range(700)], "long": [1_500_003], "none": [0, 0]}
+
+
+def make(counts, dtype, seed, gap=1, scale=1.0, head=0):
+    """Tensors that are views of one buffer: with gap 1 they start anywhere."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    starts, at = [], head
+    for n in counts:
+        at = -(-at // gap) * gap
+        starts.append(at)
+        at += n
+    flat = (torch.randn(at + 8, generator=gen, device="cuda") * scale).to(TYPES[dtype])
+    return [flat[s:s + n] for s, n in zip(starts, counts)]
+
+
+def f64(tensors):
+    return np.concatenate([t.double().cpu().numpy() for t in tensors] or [np.zeros(0)])
+
+
+def norm64(g):
+    return math.sqrt(math.fsum((g * g).tolist()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("name", sorted(LISTS))
+@pytest.mark.parametrize("gap", [1, 64])
+def test_norm(gpu, dtype, name, gap):
+    g = make(LISTS[name], dtype, 1, gap, head=gap % 64)
+    want = 0.25 * norm64(f64(g))
+    got = float(Parameters(g).grad_norm(0.25))
+    assert abs(got - want) <= 2.0 ** -23 * want
+
+
+def test_norm_of_large_and_tiny_values(gpu):
+    """Squares that fp32 could not hold."""
+    for scale in (1e30, 1e-30):
+        g = make([5000, 3], "f32", 2, scale=scale)
+        want = norm64(f64(g))
+        assert abs(float(Parameters(g).grad_norm()) - want) <= 2.0 ** -23 * want
+
+
+def test_empty_list(gpu):
+    p = Parameters([])
+    assert float(p.grad_norm()) == 0 and float(p.clip(1.0)) == 0
+    assert float(p.adamw(0.1)) == 0 and int(p.step) == 1
+
+
+@pytest.mark.parametrize("grad,out", [("f32", "f32"), ("f16", "f32"), ("bf16", "f32"),
+                                      ("bf16", "bf16"), ("f16", "f16"), ("f32", "f16"),
+                                      ("f32", "bf16")])
+@pytest.mark.parametrize("name,gap", [("one", 1), ("model", 64), ("sizes", 1), ("sizes", 64),
+                                      ("many", 1), ("long", 1), ("long", 64), ("none", 1)])
+def test_clip(gpu, grad, out, name, gap):
+    counts = LISTS[name]
+    g, o = make(counts, grad, 3, gap, head=1 % gap), make(counts, out, 4, gap, head=3 % gap)
+    g0 = f64(g)
+    p = Parameters(g, clipped=o)
+    for max_norm, scale in ((1.0, 1.0), (0.5, 1 / 1024), (float("inf"), 2.0)):
+        norm = float(p.clip(max_norm, scale))
+        n = scale * norm64(g0)
+        assert abs(norm - n) <= 2.0 ** -23 * n
+        want = g0 * (scale * (max_norm / n if n > max_norm else 1.0))
+        extra = UNIT[out] if out != "f32" else 0.0
+        got = f64(o)
+        assert np.all(np.abs(got - want) <= np.abs(want) * (2.0 ** -22 + extra) + LEAST[out])
+        assert np.array_equal(f64(g), g0)
+
+
+def test_clip_in_place_and_within_the_norm(gpu):
+    """In place the gradients end at max_norm; within it, with scale 1, they
+    keep their bits."""
+    for dtype in ("f32", "bf16"):
+        g = make(COUNTS, dtype, 5)
+        g0 = f64(g)
+        p = Parameters(g, clipped=g)
+        n = norm64(g0)
+        p.clip(2 * n)
+        assert np.array_equal(f64(g), g0)
+        p.clip(n / 3)
+        extra = UNIT[dtype] if dtype != "f32" else 0.0
+        assert np.all(np.abs(f64(g) - g0 / 3) <= np.abs(g0) / 3 * (2.0 ** -22 + extra))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_clip_shows_gradients_that_are_not_finite(gpu, bad):
+    g = make([100, 5000], "f32", 6)
+    g[1][4321] = bad
+    o = make([100, 5000], "f32", 7)
+    norm = float(Parameters(g, clipped=o).clip(1.0))
+    got = f64(o)
+    if math.isnan(bad):
+        assert math.isnan(norm) and np.isnan(got).all()
+    else:
+        assert math.isinf(norm) and np.isnan(got[100 + 4321])
+        assert not np.delete(got, 100 + 4321).any()
+
+
+def adamw64(g, p, m, v, ema, t, lr, betas, eps, decay, f, ema_decay):
+    """New values and bounds of their fp32 errors (u = 2^-24, first order, with
+    every operation's rounding counted; twice that is taken)."""
+    u = 2.0 ** -24
+    b1, b2 = betas
+    g = g * f
+    m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    # constants and products: two roundings each, f and g f two more, then the sum
+    em = u * (2 * np.abs(b1 * m) + 4 * np.abs((1 - b1) * g) + np.abs(m1))
+    ev = u * (2 * b2 * v + 7 * (1 - b2) * g * g + v1)
+    c1, c2 = 1 / (1 - b1 ** t), 1 / (1 - b2 ** t)
+    root = np.sqrt(v1 * c2) + eps
+    d = m1 * c1 / root
+    # the root carries half of v's error, the two roundings of v c2 and its own
+    with np.errstate(divide="ignore", invalid="ignore"):
+        er = np.where(v1 > 0, ev / v1 / 2, 0) + 4 * u
+    ed = em * c1 / root + np.abs(d) * (er + 5 * u)
+    p1 = p - lr * (d + decay * p)
+    ep = lr * ed + u * (np.abs(p1) + lr * (4 * np.abs(d) + 5 * decay * np.abs(p)))
+    e1 = ema_decay * ema + (1 - ema_decay) * p1
+    ee = (1 - ema_decay) * ep + u * (2 * ema_decay * np.abs(ema) +
+                                     2 * (1 - ema_decay) * np.abs(p1) + np.abs(e1))
+    return (m1, 2 * em), (v1, 2 * ev), (p1, 2 * ep), (e1, 2 * ee)
+
+
+@pytest.mark.parametrize("dtype,with_ema,decay", [("f32", True, 0.01), ("f32", False, 0.0),
+                                                  ("f16", True, 0.0), ("bf16", False, 0.1)])
+@pytest.mark.parametrize("name,gap", [("one", 1), ("model", 64), ("sizes", 1), ("sizes", 64),
+                                      ("many", 1), ("long", 64)])
+def test_adamw(gpu, dtype, with_ema, decay, name, gap):
+    counts = LISTS[name]
+    g = make(counts, dtype, 8, gap, head=1 % gap)
+    p, m, v = (make(counts, "f32", s, gap, sc) for s, sc in ((9, 0.1), (10, 0.02), (11, 0.1)))
+    for t in v:
+        t.square_()
+    ema = make(counts, "f32", 12, gap, 0.1) if with_ema else None
+    step = torch.tensor([41], dtype=torch.int64, device="cuda")
+    lst = Parameters(g, p, m, v, ema=ema, step=step)
+    args = dict(lr=1.6e-3, betas=(0.9, 0.99), eps=1e-8)
+    for k, (max_norm, scale) in enumerate([(1.0, 1.0), (float("inf"), 0.5), (1e9, 1.0)]):
+        before = [f64(x) for x in (g, p, m, v)] + [f64(ema) if ema else np.zeros(sum(counts))]
+        n = scale * norm64(before[0])
+        norm = float(lst.adamw(weight_decay=decay, max_norm=max_norm, scale=scale,
+                               ema_decay=0.99, **args))
+        assert abs(norm - n) <= 2.0 ** -23 * n
+        assert int(step) == 42 + k
+        f = scale * (max_norm / n if n > max_norm else 1.0)
+        want = adamw64(*before, 42 + k, 1.6e-3, (0.9, 0.99), 1e-8, decay, f, 0.99)
+        for (w, err), x in zip(want, (m, v, p, ema)):
+            if x is not None:
+                off = np.abs(f64(x) - w) - err - 2.0 ** -148
+                assert off.max() <= 0, float(off.max())
+        assert np.array_equal(f64(g), before[0])
+
+
+def test_adamw_from_the_start(gpu):
+    """Zero moments, step 0: the first update has the size lr wherever g is not 0."""
+    g = make([300, 5], "f32", 13)
+    g[0][:10] = 0
+    p, m, v = ([torch.zeros_like(x) for x in g] for _ in range(3))
+    lst = Parameters(g, p, m, v)
+    lst.adamw(0.25)
+    g0, got = f64(g), f64(p)
+    assert int(lst.step) == 1
+    assert np.array_equal(got[:10], np.zeros(10))
+    assert np.allclose(got[10:], -0.25 * np.sign(g0[10:]), rtol=2e-6, atol=0)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_adamw_leaves_out_a_step_that_overflowed(gpu, bad, dtype):
+    counts = [3, 9000, 17]
+    g = make(counts, dtype, 14)
+    p, m, v, ema = (make(counts, "f32", 15 + k) for k in range(4))
+    before = [f64(x) for x in (p, m, v, ema)]
+    keep = g[1][8999].clone()
+    g[1][8999] = bad
+    lst = Parameters(g, p, m, [x.square_() for x in v], ema=ema)
+    before[2] = f64(v)
+    norm = float(lst.adamw(0.1, max_norm=1.0))
+    assert not math.isfinite(norm) and int(lst.step) == 0
+    assert all(np.array_equal(a, f64(b)) for a, b in zip(before, (p, m, v, ema)))
+    g[1][8999] = keep
+    assert math.isfinite(float(lst.adamw(0.1, max_norm=1.0))) and int(lst.step) == 1
+    assert not np.array_equal(before[0], f64(p))
+
+
+def test_results_do_not_depend_on_the_run(gpu):
+    """The same bits again: no order of additions is left to chance."""
+    outs = []
+    for _ in range(3):
+        g = make(LISTS["many"] + [2_000_001], "f32", 20)
+        p, m, v = (make(LISTS["many"] + [2_000_001], "f32", 21 + k) for k in range(3))
+        lst = Parameters(g, p, m, [x.square_() for x in v], clipped=g)
+        norms = [float(lst.grad_norm()), float(lst.clip(3.0)), float(lst.adamw(0.01, max_norm=1.0))]
+        outs.append((norms, f64(g), f64(p)))
+    for norms, a, b in outs[1:]:
+        assert norms == outs[0][0]
+        assert np.array_equal(a, outs[0][1]) and np.array_equal(b, outs[0][2])
+
+
+def test_guard_values_stay(gpu):
+    """Views in the middle of buffers: what lies around them is not touched."""
+    for start, n in [(1, 4097), (4, 8192), (3, 1), (2, 5000)]:
+        bufs = [torch.full((n + 16,), 5.0, device="cuda") for _ in range(5)]
+        g = torch.randn(n + 16, device="cuda")
+        cut = lambda b: [b[start:start + n]]
+        lst = Parameters(cut(g), *(cut(b) for b in bufs[:3]), ema=cut(bufs[3]),
+                         clipped=cut(bufs[4]))
+        lst.clip(1e-3)
+        lst.adamw(0.1, max_norm=1.0)
+        for b in bufs:
+            assert bool((b[:start] == 5).all()) and bool((b[start + n:] == 5).all())
+            assert not bool((b[start:start + n] == 5).any())
+
+
+def test_another_stream_and_a_graph(gpu):
+    """A list used on a stream of its own, and captured: the replays go on
+    counting steps and see new gradients."""
+    def lists():
+        g = make(COUNTS, "f32", 30)
+        p, m, v = (make(COUNTS, "f32", 31 + k) for k in range(3))
+        return g, p, Parameters(g, p, m, [x.square_() for x in v])
+    g1, p1, eager = lists()
+    g2, p2, other = lists()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    eager.adamw(0.01, max_norm=1.0)
+    other.adamw(0.01, max_norm=1.0, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(p1), f64(p2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other.adamw(0.01, max_norm=1.0)
+    for k in range(4):
+        for a, b in zip(g1, g2):
+            a.mul_(1.5 - 0.25 * k)
+            b.copy_(a)
+        eager.adamw(0.01, max_norm=1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(other.step) == int(eager.step) == 2 + k
+        assert float(other.norm) == float(eager.norm)
+        assert np.array_equal(f64(p1), f64(p2))
+
+
+def test_refusals(gpu):
+    x = lambda n=8, **k: torch.zeros(n, device="cuda", **k)
+    g = [x(), x(3)]
+    bad = [
+        lambda: Parameters(g, clipped=[x()]),
+        lambda: Parameters(g, clipped=[x(), x(4)]),
+        lambda: Parameters([x(dtype=torch.float64)]),
+        lambda: Parameters([x().cpu()]),
+        lambda: Parameters([x(16)[::2]]),
+        lambda: Parameters(g, params=[x(), x(3)]),
+        lambda: Parameters(g, ema=[x(), x(3)]),
+        lambda: Parameters([x()], [x(dtype=torch.float16)], [x()], [x()]),
+        lambda: Parameters([x()]).clip(1.0),
+        lambda: Parameters([x()]).adamw(0.1),
+    ]
+    for call in bad:
+        with pytest.raises(octnca.OctreeNCAError):
+            call()
+    buf = x(32)
+    for args in [dict(clipped=[buf[4:12]]), dict(params=[buf[8:16]], m=[buf[15:23]], v=[x()])]:
+        with pytest.raises(octnca.OctreeNCAError):
+            Parameters([buf[:8]], **args)
+    lst = Parameters([x()], [x()], [x()], [x()], clipped=[x()])
+    calls = [lambda: lst.clip(0.0), lambda: lst.clip(float("nan")), lambda: lst.clip(-1.0),
+             lambda: lst.clip(1.0, 0.0), lambda: lst.clip(1.0, float("inf")),
+             lambda: lst.grad_norm(float("nan")), lambda: lst.adamw(-0.1),
+             lambda: lst.adamw(0.1, betas=(1.0, 0.99)), lambda: lst.adamw(0.1, betas=(0.9, -0.1)),
+             lambda: lst.adamw(0.1, eps=0.0), lambda: lst.adamw(0.1, weight_decay=-1.0),
+             lambda: lst.adamw(0.1, max_norm=0.0), lambda: lst.adamw(float("nan")),
+             lambda: lst.adamw(0.1, ema_decay=1.5)]
+    for call in calls:
+        with pytest.raises(octnca.OctreeNCAError) as e:
+            call()
+        assert e.value.status == octnca.OCTNCA_EINVAL
+    assert int(lst.step) == 0

@@ -1,0 +1,325 @@
+"""The 8-bit state cache against its definition in 64 bits.
+
+Bounds.  I8: code = rint(fl(x r)), r = fl(127 / a): x r carries two roundings of
+2^-24 relative, at most 127 * 2^-23 in all, so a code is within 0.5 + 127 * 2^-23
+of x 127 / a (2^-22 taken); the scale a / 127 is rounded once (2^-24).  F8: the scale is a
+power of two and x / scale exact, so scale and code are those of the definition
+bit for bit.  Reading multiplies in fp32, one rounding, and rounds once more to
+fp16 states."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2508_06993_amd as octnca
+from paper_2508_06993_amd.runtime import StateCache
+
+pytestmark = pytest.mark.gpu
+
+HIDDEN = {12: 48, 16: 64, 20: 100}
+TINY = 2.0 ** -100
+NP = {"f32": np.float32, "f16": np.float16}
+
+
+def model(c=16, dtype="f32"):
+    return octnca.Model(ndim=3, n_in=3, dtype=dtype, channels=c, hidden=HIDDEN[c])
+
+
+def states(seed, n, extent, c, dtype):
+    """Channels of very different magnitude, a smooth part and noise."""
+    rng = np.random.default_rng(seed)
+    x = rng.normal(0, 1, (n,) + extent + (c,)) * np.exp2(np.linspace(-4, 7, c))
+    x[..., :3] = rng.uniform(0, 1, (n,) + extent + (3,))
+    return x.astype(NP[dtype])
+
+
+def e4m3_values():
+    """Value of each of the 256 codes, from the format's definition."""
+    code = np.arange(256)
+    e, f = (code >> 3) & 15, code & 7
+    v = np.where(e > 0, (1 + f / 8.0) * np.exp2(e - 7.0), f / 8.0 * 2.0 ** -6)
+    v[(code & 127) == 127] = np.nan
+    return np.where(code >> 7, -v, v)
+
+
+def e4m3_round(y):
+    """Nearest e4m3 value, ties to the even code, of |y| <= 448."""
+    v = e4m3_values()[:127]
+    k = np.clip(np.searchsorted(v, np.abs(y)), 1, 126)
+    lo, hi = np.abs(y) - v[k - 1], v[k] - np.abs(y)
+    pick = np.where((lo < hi) | ((lo == hi) & ((k - 1) % 2 == 0)), k - 1, k)
+    return np.copysign(v[pick], y)
+
+
+def blocks_of(x, block):
+    """[cells][C] -> list of [<= block][C]."""
+    return [x[i:i + block] for i in range(0, len(x), block)]
+
+
+def check_block(x, code, scale, back, kind, dtype):
+    """One block's codes [cells][C], scales [C] and read values against x."""
+    x = x.astype(np.float64)
+    fine = np.isfinite(x)
+    a = np.maximum(np.where(fine, np.abs(x), 0).max(0), TINY)
+    scale = scale.astype(np.float64)
+    if kind == "i8":
+        assert np.all(np.abs(scale * 127 / a - 1) <= 2.0 ** -23)
+        code = code.astype(np.int8)
+        assert np.all(code[~fine] == -128)
+        off = np.abs(code - np.where(fine, x, 0) * 127 / a)[fine]
+        assert off.size == 0 or off.max() <= 0.5 + 127 * 2.0 ** -22
+        value = np.where(code == -128, np.nan, code * scale)
+    else:
+        k = np.round(np.log2(scale))
+        assert np.array_equal(scale, np.exp2(k))
+        assert np.all(a / scale <= 448) and np.all(a / (scale / 2) > 448)
+        code = code.astype(np.uint8)
+        got = e4m3_values()[code]
+        assert np.all((code & 127)[~fine] == 127)
+        want = e4m3_round(np.where(fine, x, 0) / scale)
+        assert np.array_equal(got[fine], want[fine])
+        value = got * scale
+    with np.errstate(over="ignore"):
+        want = value.astype(np.float32).astype(NP[dtype])
+    assert np.array_equal(back, want, equal_nan=True)
+
+
+def roundtrip(x, kind, block, c, dtype, slots=None, n_slots=None):
+    """(codes, scales, values read back) of states x [n][d][h][w][C]."""
+    n, extent = x.shape[0], x.shape[1:4]
+    cache = StateCache(model(c, dtype), extent, n_slots or n, kind, block)
+    at = None if slots is None else torch.tensor(slots, dtype=torch.int64, device="cuda")
+    cache.write(torch.from_numpy(x).cuda(), at)
+    out = torch.full(x.shape, 7.0, dtype=model(c, dtype).torch_dtype, device="cuda")
+    cache.read(out, at)
+    return cache, out.cpu().numpy()
+
+
+def check_all(x, cache, back, kind, block, c, dtype, slots=None):
+    codes, scales = cache.buffers.codes.cpu().numpy(), cache.buffers.scales.cpu().numpy()
+    for i in range(len(x)):
+        s = i if slots is None else slots[i]
+        parts = zip(blocks_of(x[i].reshape(-1, c), block), blocks_of(codes[s], block), scales[s],
+                    blocks_of(back[i].reshape(-1, c), block))
+        for xb, cb, sb, bb in parts:
+            check_block(xb, cb, sb, bb, kind, dtype)
+
+
+EXTENTS = [(1, 1, 1), (1, 1, 7), (1, 8, 8), (1, 9, 15), (3, 11, 13), (1, 40, 50)]
+
+
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+@pytest.mark.parametrize("block", [32, 64, 128])
+@pytest.mark.parametrize("c,dtype", [(16, "f32"), (16, "f16"), (12, "f32"), (12, "f16"),
+                                     (20, "f32"), (20, "f16")])
+def test_codes_scales_and_values(gpu, kind, block, c, dtype):
+    for extent in EXTENTS:
+        x = states(5, 2, extent, c, dtype)
+        cache, back = roundtrip(x, kind, block, c, dtype)
+        check_all(x, cache, back, kind, block, c, dtype)
+
+
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+@pytest.mark.parametrize("c,dtype", [(16, "f32"), (20, "f16"), (12, "f32")])
+def test_values_that_are_not_finite_and_extreme_ones(gpu, kind, c, dtype):
+    big = float(np.finfo(NP[dtype]).max)
+    small = float(np.finfo(NP[dtype]).smallest_subnormal)
+    x = states(6, 1, (1, 20, 20), c, dtype).reshape(400, c)
+    x[3, 0], x[70, 0], x[71, 0] = np.nan, np.inf, -np.inf
+    x[64:128, 1] = np.nan                   # a block of one channel with nothing finite
+    x[0:64, 2], x[5, 2] = 0, np.inf         # and one with zeros beside an infinity
+    x[128:192, 3] = -big                    # the type's lowest value
+    x[200, 4] = big                         # one value that all others vanish beside
+    x[256:320, 5] = small
+    x[256:320, 6] = np.where(np.arange(64) % 2, small, 0)
+    x[320:384, 7] = 0
+    x[300, 8] = -np.nan
+    cache, back = roundtrip(x.reshape(1, 1, 20, 20, c), kind, 64, c, dtype)
+    check_all(x.reshape(1, 1, 20, 20, c), cache, back, kind, 64, c, dtype)
+
+
+@pytest.mark.parametrize("kind", ["i8", "f8"])
+def test_ties_go_to_even(gpu, kind):
+    """Values half way between two codes, exact in fp32: with a = 127 (I8) and
+    448 (F8) both factors are 1."""
+    x = np.zeros((64, 16), np.float32)
+    if kind == "i8":
+        x[:62, :] = (np.arange(62) - 31 + 0.5)[:, None]
+        x[63] = 127
+    else:
+        v = e4m3_values()[:127]
+        x[:62, :] = ((v[40:102] + v[41:103]) / 2)[:, None] * np.where(np.arange(16) % 2, 1, -1)
+        x[63] = 448
+    cache, back = roundtrip(x.reshape(1, 1, 8, 8, 16), kind, 64, 16, "f32")
+    want = np.rint(x) if kind == "i8" else e4m3_round(x)
+    assert np.array_equal(back.reshape(64, 16), want.astype(np.float32))
+
+
+@pytest.mark.parametrize("c,dtype,kind", [(16, "f32", "i8"), (12, "f16", "f8"), (20, "f32", "f8")])
+def test_slots_in_any_order(gpu, c, dtype, kind):
+    x = states(8, 5, (2, 7, 9), c, dtype)
+    slots = [6, 0, 3, 8, 1]
+    cache, back = roundtrip(x, kind, 32, c, dtype, slots, 9)
+    check_all(x, cache, back, kind, 32, c, dtype, slots)
+    untouched = [s for s in range(9) if s not in slots]
+    assert not cache.buffers.codes[untouched].any() and not cache.buffers.scales[untouched].any()
+
+
+def test_slots_outside_the_cache_and_given_twice(gpu):
+    """Entries outside are not written and read as zeros; of equal entries the
+    last state is kept, and all of them read it."""
+    x = states(9, 6, (1, 11, 30), 16, "f32")
+    slots = [2, -1, 2, 4, 1 << 40, 2]
+    cache, back = roundtrip(x, "i8", 64, 16, "f32", slots, 4)
+    one, alone = roundtrip(x[5:], "i8", 64, 16, "f32", [2], 4)
+    assert torch.equal(cache.buffers.codes, one.buffers.codes)
+    assert torch.equal(cache.buffers.scales, one.buffers.scales)
+    for i, s in enumerate(slots):
+        assert np.array_equal(back[i], alone[0] if s == 2 else np.zeros_like(alone[0]))
+
+
+def test_many_states_with_equal_slots(gpu):
+    """More states than a wavefront has lanes, most slots given several times."""
+    rng = np.random.default_rng(3)
+    x = states(10, 150, (1, 3, 13), 16, "f32")
+    slots = rng.integers(-3, 23, 150)
+    cache, back = roundtrip(x, "i8", 32, 16, "f32", slots.tolist(), 20)
+    last = {int(s): i for i, s in enumerate(slots)}
+    alone, _ = roundtrip(x, "i8", 32, 16, "f32")
+    for i, s in enumerate(slots):
+        if 0 <= s < 20:
+            assert torch.equal(cache.buffers.codes[s], alone.buffers.codes[last[int(s)]])
+            assert torch.equal(cache.buffers.scales[s], alone.buffers.scales[last[int(s)]])
+        else:
+            assert not back[i].any()
+
+
+def test_an_empty_cache_reads_zeros(gpu):
+    cache = StateCache(model(), (1, 4, 4), 0)
+    x = torch.ones((2, 1, 4, 4, 16), device="cuda")
+    at = torch.tensor([0, 5], dtype=torch.int64, device="cuda")
+    cache.write(x, at)
+    cache.read(x, at)
+    assert not x.any()
+
+
+@pytest.mark.parametrize("c,dtype,kind", [(16, "f32", "i8"), (20, "f16", "i8"), (12, "f32", "f8")])
+def test_a_long_state_in_pieces(gpu, c, dtype, kind):
+    """Written and read in pieces, a state is what it is written whole; a read
+    may end anywhere."""
+    x = states(11, 1, (1, 1, 1000), c, dtype)
+    whole, back = roundtrip(x, kind, 64, c, dtype)
+    cache = StateCache(model(c, dtype), (1, 1, 1000), 2, kind, 64)
+    dev = torch.from_numpy(x).cuda()
+    for lo, hi in [(640, 1000), (0, 64), (64, 640), (1000, 1000)] if 1000 % 64 == 0 else \
+            [(640, 1000), (0, 64), (64, 640)]:
+        cache.write(dev[:, :, :, lo:hi].contiguous(), first=1, from_cell=lo)
+    assert torch.equal(cache.buffers.codes[1], whole.buffers.codes[0])
+    assert torch.equal(cache.buffers.scales[1], whole.buffers.scales[0])
+    assert not cache.buffers.codes[0].any()
+    for lo, hi in [(0, 1), (64, 65), (128, 1000), (576, 703)]:
+        out = torch.zeros((1, 1, 1, hi - lo, c), dtype=model(c, dtype).torch_dtype, device="cuda")
+        cache.read(out, first=1, from_cell=lo)
+        assert np.array_equal(out.cpu().numpy(), back[:, :, :, lo:hi])
+
+
+def test_no_states_and_no_cells(gpu):
+    cache = StateCache(model(), (1, 8, 8), 2)
+    cache.buffers.codes.fill_(3)
+    cache.write(torch.zeros((0, 1, 8, 8, 16), device="cuda"))
+    cache.write(torch.zeros((2, 1, 0, 8, 16), device="cuda"))
+    cache.read(torch.zeros((2, 1, 0, 8, 16), device="cuda"))
+    cache.read(torch.zeros((0, 1, 8, 8, 16), device="cuda"))
+    assert bool((cache.buffers.codes == 3).all())
+
+
+def test_guard_bytes_stay(gpu):
+    """Nothing outside the addressed cells is written."""
+    for c, dtype in [(16, "f32"), (12, "f16"), (20, "f32")]:
+        x = torch.from_numpy(states(12, 3, (1, 5, 17), c, dtype)).cuda()
+        cache = StateCache(model(c, dtype), (1, 5, 17), 5, "i8", 32)
+        cache.buffers.codes.fill_(77)
+        cache.buffers.scales.fill_(-1)
+        cache.write(x, first=1)
+        for s in (0, 4):
+            assert bool((cache.buffers.codes[s] == 77).all())
+            assert bool((cache.buffers.scales[s] == -1).all())
+        buf = torch.full((5,) + tuple(x.shape[1:]), float("nan"), dtype=x.dtype, device="cuda")
+        cache.read(buf[1:4], first=1)
+        assert bool(buf[0].isnan().all()) and bool(buf[4].isnan().all())
+        assert not bool(buf[1:4].isnan().any())
+
+
+def test_offsets_past_32_bits(gpu):
+    """Slot 4 of states of 2^26 cells starts past 2^32 bytes of codes; so does
+    the second state in fp32."""
+    cells = 1 << 26
+    cache = StateCache(model(), (64, 1024, 1024), 5)
+    x = torch.zeros((2, 64, 1024, 1024, 16), device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    part = torch.randn((cells // 64, 16), generator=gen, device="cuda")
+    x[1].view(cells, 16)[-len(part):] = part
+    x[0].view(cells, 16)[:len(part)] = part
+    cache.write(x, torch.tensor([0, 4], dtype=torch.int64, device="cuda"))
+    assert torch.equal(cache.buffers.codes[0, :len(part)], cache.buffers.codes[4, -len(part):])
+    assert not cache.buffers.codes[1:4].any() and not cache.buffers.codes[4, :-len(part)].any()
+    want = x[1].clone()
+    x.fill_(9)
+    cache.read(x, torch.tensor([1, 4], dtype=torch.int64, device="cuda"))
+    assert not x[0].any()
+    assert float((x[1] - want).abs().max()) <= float(part.abs().max()) / 254 * 1.001
+
+
+def test_another_stream_and_a_graph(gpu):
+    """Calls on a stream of their own, and captured into a graph that is
+    replayed with new contents."""
+    x = states(13, 2, (2, 9, 21), 16, "f32")
+    _, want = roundtrip(x, "i8", 64, 16, "f32")
+    cache = StateCache(model(), (2, 9, 21), 2)
+    src, out = torch.from_numpy(x).cuda(), torch.zeros(x.shape, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    cache.write(src, stream=side)
+    cache.read(out, stream=side)
+    side.synchronize()
+    assert np.array_equal(out.cpu().numpy(), want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.write(src)
+        cache.read(out)
+    for k in range(3):
+        new = states(20 + k, 2, (2, 9, 21), 16, "f32")
+        src.copy_(torch.from_numpy(new))
+        out.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(out.cpu().numpy(), roundtrip(new, "i8", 64, 16, "f32")[1])
+
+
+def test_refusals(gpu):
+    m = model()
+    with pytest.raises(ValueError):
+        StateCache(m, (1, 8, 8), 2, code="i4")
+    with pytest.raises(ValueError):
+        StateCache(m, (1, 8, 8), 2, block=48)
+    with pytest.raises(octnca.OctreeNCAError):
+        StateCache(m, (1, 8, 8), 2, scales=torch.zeros((2, 3, 16), device="cuda"))
+    with pytest.raises(octnca.OctreeNCAError):
+        StateCache(m, (1, 8, 8), 2, codes=torch.zeros((2, 64, 16), device="cuda"))
+    cache = StateCache(m, (1, 8, 8), 2)
+    x = torch.zeros((1, 1, 8, 8, 16), device="cuda")
+    bad = [
+        lambda: cache.write(x.half()), lambda: cache.write(x.cpu()),
+        lambda: cache.write(x.transpose(2, 3).contiguous().transpose(2, 3)[:, :, :, ::2]),
+        lambda: cache.write(x[..., :12].contiguous()),
+        lambda: cache.write(x, first=2), lambda: cache.write(x, first=-1),
+        lambda: cache.write(x, from_cell=64), lambda: cache.write(x, from_cell=1),
+        lambda: cache.read(torch.zeros((3, 1, 8, 8, 16), device="cuda")),
+        lambda: cache.write(x, torch.zeros(2, dtype=torch.int64, device="cuda")),
+        lambda: cache.write(x, torch.zeros(1, dtype=torch.int32, device="cuda")),
+        lambda: cache.write(torch.zeros(1025, device="cuda")[1:].view(1, 1, 8, 8, 16)),
+        lambda: StateCache(m, (1, 1, 200), 1).write(torch.zeros((1, 100, 16), device="cuda")),
+    ]
+    for call in bad:
+        with pytest.raises(octnca.OctreeNCAError):
+            call()
+    assert not cache.buffers.codes.any()
