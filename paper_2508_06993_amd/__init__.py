@@ -10,6 +10,7 @@ missing, every call raises ``OctreeNCAError``.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -29,7 +30,7 @@ __all__ = [
     "octree_nca_step_backward_workspace_bytes", "octree_nca_step_backward",
     "octree_nca_upsample_backward", "octree_nca_readout_mse_workspace_bytes",
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
-    "level_grads_struct", "StateCacheBuffers", "octree_nca_state_cache_write",
+    "level_grads_struct", "StateCacheBuffers", "state_cache_refs", "octree_nca_state_cache_write",
     "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
     "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
     "octree_nca_adamw", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
@@ -276,7 +277,9 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
 
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current stream's handle; torch.cuda.current_stream() would also
+        # make a Stream object, 2.7 us a call
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
@@ -561,7 +564,7 @@ def octree_nca_train_step(model: Model, image, factors, weights, steps, fire_rat
 # state cache: states in 8 bits
 # ---------------------------------------------------------------------------
 
-@dataclass
+@dataclass(frozen=True)
 class StateCacheBuffers:
     """A cache's description and device memory (octnca_state_cache): codes int8
     or uint8 [slots][cells][C], scales fp32 [slots][ceil(cells / block)][C]."""
@@ -590,36 +593,38 @@ class StateCacheBuffers:
                            _ptr(self.scales, torch.float32, "scales"))
 
 
-def _cache_call(name, model, cache, states, from_cell, slots, first, stream):
-    """states: [n][cells...][C]; n = the slots named by ``slots`` (int64 tensor),
-    or the states' first axis."""
-    n, c = states.shape[0], states.shape[-1]
+def _cache_call(name, model, refs, states, from_cell, slots, first, stream):
+    """states: [n][cells...][C]; refs: the model's and the cache's structs by reference."""
+    shape = states.shape
+    n, c = shape[0], shape[-1]
     if c != model.channels:
         raise OctreeNCAError(f"states: expected {model.channels} channels, got {c}")
     if slots is not None and tuple(slots.shape) != (n,):
         raise OctreeNCAError(f"slots: expected shape {(n,)}, got {tuple(slots.shape)}")
-    count = 1
-    for v in states.shape[1:-1]:
-        count *= v
-    st = getattr(lib(), name)(ctypes.byref(model.struct()), ctypes.byref(cache.struct(model)),
-                              _ptr(states, model.torch_dtype, "states"), int(from_cell), count, n,
-                              _ptr(slots, torch.int64, "slots"), int(first), _stream(stream))
+    st = getattr(lib(), name)(*refs, _ptr(states, model.torch_dtype, "states"), int(from_cell),
+                              math.prod(shape[1:-1]), n, _ptr(slots, torch.int64, "slots"),
+                              int(first), _stream(stream))
     _check(st, name)
 
 
+def state_cache_refs(model: Model, cache: StateCacheBuffers):
+    """The two structs of a call; a caller of many keeps them."""
+    return ctypes.byref(model.struct()), ctypes.byref(cache.struct(model))
+
+
 def octree_nca_state_cache_write(model: Model, cache: StateCacheBuffers, states, from_cell=0,
-                                 slots=None, first=0, stream=None) -> None:
+                                 slots=None, first=0, stream=None, refs=None) -> None:
     """Quantise states [n][...cells][C] into the slots ``slots`` (device int64
     [n]) or first, first + 1, ..."""
-    _cache_call("octree_nca_state_cache_write", model, cache, states, from_cell, slots, first,
-                stream)
+    _cache_call("octree_nca_state_cache_write", model, refs or state_cache_refs(model, cache),
+                states, from_cell, slots, first, stream)
 
 
 def octree_nca_state_cache_read(model: Model, cache: StateCacheBuffers, states, from_cell=0,
-                                slots=None, first=0, stream=None) -> None:
+                                slots=None, first=0, stream=None, refs=None) -> None:
     """Fill states [n][...cells][C] with the values of the slots."""
-    _cache_call("octree_nca_state_cache_read", model, cache, states, from_cell, slots, first,
-                stream)
+    _cache_call("octree_nca_state_cache_read", model, refs or state_cache_refs(model, cache),
+                states, from_cell, slots, first, stream)
 
 
 # ---------------------------------------------------------------------------

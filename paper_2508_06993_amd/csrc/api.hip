@@ -1274,7 +1274,7 @@ int check_params(const octnca_param *params, int32_t n, octnca_param_list *l) {
         any = true;
         l->has = has;
         l->elements += t.count;
-        l->chunks += (t.count + kParamChunk - 1) / kParamChunk;
+        l->chunks += param_chunks(t);
         if (l->elements > kMaxCells) return OCTNCA_ESHAPE;
     }
     return OCTNCA_OK;

@@ -228,6 +228,7 @@ hipError_t launch_cache_read(Dtype dt, const CacheArgs &a, void *states, hipStre
 // tensor.  param_has_*: which arrays the list's tensors have.
 constexpr int kParamChunk = 4096;
 enum : int32_t { kHasClipped = 1, kHasParam = 2, kHasEma = 4 };
+int64_t param_chunks(const octnca_param &t);   // of one tensor
 size_t param_table_bytes(int64_t chunks);
 hipError_t launch_param_table(const octnca_param *params, int n, void *table, hipStream_t stream);
 // Sum of squares of all gradients (table scratch), then what it is for.

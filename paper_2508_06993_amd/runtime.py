@@ -13,7 +13,8 @@ import torch
 from . import (Model, StateCacheBuffers, octree_nca_adamw, octree_nca_clip_grads,
                octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
                octree_nca_param_table_bytes, octree_nca_state_cache_read,
-               octree_nca_state_cache_write, octree_nca_workspace_bytes, param_structs)
+               octree_nca_state_cache_write, octree_nca_workspace_bytes, param_structs,
+               state_cache_refs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
 
@@ -85,7 +86,7 @@ class StateCache:
         if scales is None:
             scales = torch.zeros((slots, -(-cells // block), c), device=device)
         self.buffers = StateCacheBuffers(codes, scales, cells, code, block)
-        self.buffers.struct(model)      # checks the description
+        self.refs = state_cache_refs(model, self.buffers)
 
     def write(self, states: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0,
               from_cell=0, stream=None) -> None:
@@ -93,12 +94,13 @@ class StateCache:
         ``slots``: device int64 [n], entries outside the cache are left out; or
         None for slots first, first + 1, ..."""
         octree_nca_state_cache_write(self.model, self.buffers, states, from_cell, slots, first,
-                                     stream)
+                                     stream, self.refs)
 
     def read(self, out: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0, from_cell=0,
              stream=None) -> torch.Tensor:
         """Fills and returns ``out`` [n][...][C]; slots outside the cache read as zeros."""
-        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first, stream)
+        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first, stream,
+                                    self.refs)
         return out
 
 
