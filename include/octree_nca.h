@@ -507,7 +507,9 @@ typedef struct {
     void *table;
     int64_t chunks;
     int64_t elements;
-    int32_t has;          /* bit 0 clipped, bit 1 param / m / v, bit 2 ema */
+    int64_t bytes;        /* of all arrays */
+    int32_t has;          /* bit 0 clipped, bit 1 param / m / v, bit 2 ema, bit 3: a clipped
+                             is its grad */
 } octnca_param_list;
 
 /* Bytes of table that a list needs (0 if the list is invalid). */

@@ -132,7 +132,8 @@ class _Param(ctypes.Structure):
 
 class _ParamList(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64),
-                ("elements", ctypes.c_int64), ("has", ctypes.c_int32)]
+                ("elements", ctypes.c_int64), ("bytes", ctypes.c_int64),
+                ("has", ctypes.c_int32)]
 
 
 class _AdamW(ctypes.Structure):

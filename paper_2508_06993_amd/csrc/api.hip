@@ -1250,7 +1250,7 @@ bool misaligned(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
 int check_params(const octnca_param *params, int32_t n, octnca_param_list *l) {
     if (n < 0 || (n > 0 && params == nullptr)) return OCTNCA_EINVAL;
     l->table = nullptr;
-    l->chunks = l->elements = 0;
+    l->chunks = l->elements = l->bytes = 0;
     l->has = 0;
     bool any = false;
     for (int32_t i = 0; i < n; ++i) {
@@ -1270,10 +1270,13 @@ int check_params(const octnca_param *params, int32_t n, octnca_param_list *l) {
             return OCTNCA_EINVAL;
         const int32_t has = (t.clipped ? kHasClipped : 0) | (t.param ? kHasParam : 0) |
                             (t.ema ? kHasEma : 0);
-        if (any && has != l->has) return OCTNCA_EINVAL;
+        if (any && has != (l->has & ~kHasInPlace)) return OCTNCA_EINVAL;
         any = true;
-        l->has = has;
+        l->has |= has | (t.clipped == t.grad ? kHasInPlace : 0);
         l->elements += t.count;
+        l->bytes += t.count * (int64_t)(dtype_bytes(t.grad_dtype) +
+                                        (t.clipped ? dtype_bytes(t.clipped_dtype) : 0) +
+                                        (t.param ? 12 : 0) + (t.ema ? 4 : 0));
         l->chunks += param_chunks(t);
         if (l->elements > kMaxCells) return OCTNCA_ESHAPE;
     }

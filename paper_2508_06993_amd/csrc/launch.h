@@ -218,6 +218,7 @@ struct CacheArgs {
     int64_t first;
     int n, block, channels;
     bool f8;
+    bool stream;            // set by the launch: past the last-level cache
 };
 hipError_t launch_cache_write(Dtype dt, const CacheArgs &a, const void *states,
                               hipStream_t stream);
@@ -227,7 +228,7 @@ hipError_t launch_cache_read(Dtype dt, const CacheArgs &a, void *states, hipStre
 // call followed by the chunks: pieces of at most kParamChunk elements of one
 // tensor.  param_has_*: which arrays the list's tensors have.
 constexpr int kParamChunk = 4096;
-enum : int32_t { kHasClipped = 1, kHasParam = 2, kHasEma = 4 };
+enum : int32_t { kHasClipped = 1, kHasParam = 2, kHasEma = 4, kHasInPlace = 8 };
 int64_t param_chunks(const octnca_param &t);   // of one tensor
 size_t param_table_bytes(int64_t chunks);
 hipError_t launch_param_table(const octnca_param *params, int n, void *table, hipStream_t stream);

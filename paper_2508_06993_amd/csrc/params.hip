@@ -2,6 +2,7 @@
 // octree_nca.h).  The list's tensors are cut into chunks of at most kParamChunk
 // elements, each with a record in the list's table.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 
@@ -29,8 +30,11 @@ struct Chunk {
     void *clipped;
     float *param, *m, *v, *ema;
     int32_t first, end;
-    int16_t grad_dtype, clipped_dtype;
+    int32_t types;             // grad_dtype, clipped_dtype << 8
     int32_t quads;             // whether the arrays lie alike
+
+    __device__ __forceinline__ int grad_dtype() const { return types & 0xff; }
+    __device__ __forceinline__ int clipped_dtype() const { return types >> 8; }
 };
 static_assert(sizeof(Chunk) == 64 && sizeof(Scratch) % 64 == 0, "one record per 64-byte line");
 
@@ -87,8 +91,7 @@ __global__ __launch_bounds__(kThreads) void fill_table(FillArgs f, Scratch *scra
             c.first = k == 0 ? (int32_t)skip : 0;
             const int64_t left = total - k * kParamChunk;
             c.end = (int32_t)(left < kParamChunk ? left : kParamChunk);
-            c.grad_dtype = (int16_t)t.grad_dtype;
-            c.clipped_dtype = (int16_t)t.clipped_dtype;
+            c.types = t.grad_dtype | (t.clipped ? t.clipped_dtype << 8 : 0);
             c.quads = lead >= 0;
             chunks[at + k] = c;
         }
@@ -104,8 +107,28 @@ __device__ __forceinline__ uint32_t to_bf16(float x) {
     return x != x ? 0x7fc0u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
 }
 
-// Element and group-of-four access to an array of type DT.
+// Addresses read from a table are global ones (the compiler cannot know, and
+// flat accesses would wait on the LDS counter too).
+#define OCTNCA_GLOBAL __attribute__((address_space(1)))
+typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+template <typename T, bool STREAM = false>
+__device__ __forceinline__ T get(const void *p, int i) {
+    const OCTNCA_GLOBAL T *at = (const OCTNCA_GLOBAL T *)p + i;
+    return STREAM ? __builtin_nontemporal_load(at) : *at;
+}
+template <bool STREAM = false, typename T>
+__device__ __forceinline__ void put(void *p, int i, T x) {
+    OCTNCA_GLOBAL T *at = (OCTNCA_GLOBAL T *)p + i;
+    if (STREAM)
+        __builtin_nontemporal_store(x, at);
+    else
+        *at = x;
+}
+
+// An array's elements by type: Raw is a group of four as stored.
 template <int DT> struct Array {
+    using Raw = Words2;
     static __device__ __forceinline__ float value(uint32_t u) {
         return DT == OCTNCA_BF16 ? __uint_as_float(u << 16)
                                  : __half2float(__ushort_as_half((unsigned short)u));
@@ -114,32 +137,35 @@ template <int DT> struct Array {
         return DT == OCTNCA_BF16 ? to_bf16(x) : (uint32_t)__half_as_ushort(__float2half_rn(x));
     }
     static __device__ __forceinline__ float load(const void *p, int i) {
-        return value(((const uint16_t *)p)[i]);
+        return value(get<uint16_t>(p, i));
     }
     static __device__ __forceinline__ void store(void *p, int i, float x) {
-        ((uint16_t *)p)[i] = (uint16_t)bits(x);
+        put(p, i, (uint16_t)bits(x));
     }
-    static __device__ __forceinline__ float4 load4(const void *p, int q) {
-        const uint2 u = ((const uint2 *)p)[q];
-        return make_float4(value(u.x & 0xffffu), value(u.x >> 16), value(u.y & 0xffffu),
-                           value(u.y >> 16));
+    static __device__ __forceinline__ void unpack(Raw u, float *x) {
+        x[0] = value(u.x & 0xffffu);
+        x[1] = value(u.x >> 16);
+        x[2] = value(u.y & 0xffffu);
+        x[3] = value(u.y >> 16);
     }
-    static __device__ __forceinline__ void store4(void *p, int q, const float *x) {
-        ((uint2 *)p)[q] = make_uint2(bits(x[0]) | bits(x[1]) << 16, bits(x[2]) | bits(x[3]) << 16);
+    static __device__ __forceinline__ Raw pack(const float *x) {
+        return Raw{bits(x[0]) | bits(x[1]) << 16, bits(x[2]) | bits(x[3]) << 16};
     }
 };
 template <> struct Array<OCTNCA_F32> {
-    static __device__ __forceinline__ float load(const void *p, int i) {
-        return ((const float *)p)[i];
+    using Raw = Words4;
+    static __device__ __forceinline__ float load(const void *p, int i) { return get<float>(p, i); }
+    static __device__ __forceinline__ void store(void *p, int i, float x) { put(p, i, x); }
+    static __device__ __forceinline__ void unpack(Raw u, float *x) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(u[k]);
     }
-    static __device__ __forceinline__ void store(void *p, int i, float x) { ((float *)p)[i] = x; }
-    static __device__ __forceinline__ float4 load4(const void *p, int q) {
-        return ((const float4 *)p)[q];
-    }
-    static __device__ __forceinline__ void store4(void *p, int q, const float *x) {
-        ((float4 *)p)[q] = make_float4(x[0], x[1], x[2], x[3]);
+    static __device__ __forceinline__ Raw pack(const float *x) {
+        return Raw{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                   __float_as_uint(x[3])};
     }
 };
+using F32 = Array<OCTNCA_F32>;
 
 // Calls f with the type of a gradient as a constant.
 template <typename F> __device__ __forceinline__ void with_type(int dtype, F f) {
@@ -170,23 +196,44 @@ template <int T> __device__ __forceinline__ double block_sum(double s) {
     return s;
 }
 
-// Runs body over the groups of four of a chunk (element index 4 q): `whole`
-// for those inside it, `edge` per element for the two partial ones; with
-// arrays that lie differently `edge` for every element, lane after lane.
-// Thread `t` of T.
-template <int T, typename Whole, typename Edge>
-__device__ __forceinline__ void for_elements(const Chunk &c, int t, Whole whole, Edge edge) {
+// The whole groups of four of a chunk (group q: elements 4 q .. 4 q + 3 from its
+// pointers) by thread t of T, N groups of a thread at a time: load(k, q) of
+// all of them before finish(k, q), so that N loads of an array are in flight.
+template <int T, int N, typename Load, typename Finish>
+__device__ __forceinline__ void for_groups(const Chunk &c, int t, Load load, Finish finish) {
+    if (!c.quads) return;
+    const int inner = (c.first + 3) / 4, outer = c.end / 4;   // whole ones: inner .. outer - 1
+    if (inner == 0 && outer == kParamChunk / 4) {             // a full chunk: no comparisons
+#pragma unroll
+        for (int q0 = 0; q0 < kParamChunk / 4; q0 += N * T) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) load(k, q0 + k * T + t);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < N; ++k) finish(k, q0 + k * T + t);
+        }
+        return;
+    }
+    for (int q0 = t; q0 < outer; q0 += N * T) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (q0 + k * T >= inner && q0 + k * T < outer) load(k, q0 + k * T);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (q0 + k * T >= inner && q0 + k * T < outer) finish(k, q0 + k * T);
+    }
+}
+
+// The other elements: at most three before and three after the whole groups,
+// or all, lane after lane, where the arrays lie differently.
+template <int T, typename Edge>
+__device__ __forceinline__ void for_edges(const Chunk &c, int t, Edge edge) {
     if (!c.quads) {
         for (int i = t; i < c.end; i += T) edge(i);
         return;
     }
-    const int inner = (c.first + 3) / 4, outer = c.end / 4;   // whole groups inner .. outer - 1
-#pragma unroll
-    for (int k = 0; k < kParamChunk / 4 / T; ++k) {
-        const int q = t + k * T;
-        if (q >= inner && q < outer) whole(q);
-    }
-    if (t < 8) {   // the elements before and after them, at most three each
+    const int inner = (c.first + 3) / 4, outer = c.end / 4;
+    if (t < 8) {
         const int i = t < 4 ? c.first + t : std::max(outer, inner) * 4 + t - 4;
         const int stop = t < 4 ? std::min(inner * 4, c.end) : c.end;
         if (i < stop) edge(i);
@@ -198,37 +245,41 @@ __device__ __forceinline__ void for_elements(const Chunk &c, int t, Whole whole,
 // A chunk's squares in fp64 (no square of an fp32 value overflows it), by
 // thread t of T.
 template <int T> __device__ __forceinline__ double chunk_squares(const Chunk &c, int t) {
+    constexpr int kN = kParamChunk / 4 / T < 8 ? kParamChunk / 4 / T : 8;
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    with_type(c.grad_dtype, [&](auto type) {
+    with_type(c.grad_dtype(), [&](auto type) {
         using G = Array<decltype(type)::value>;
-        if (c.quads) {
-            constexpr int kN = kParamChunk / 4 / T < 8 ? kParamChunk / 4 / T : 8;
-            const int inner = (c.first + 3) / 4, outer = c.end / 4;
-            for (int q0 = 0; q0 < kParamChunk / 4; q0 += kN * T) {
-                if (q0 >= outer) break;
-                float4 g[kN];
+        typename G::Raw g[kN];
+        for_groups<T, kN>(
+            c, t, [&](int k, int q) { g[k] = get<typename G::Raw>(c.grad, q); },
+            [&](int k, int) {
+                float x[4];
+                G::unpack(g[k], x);
 #pragma unroll
-                for (int k = 0; k < kN; ++k) {
-                    const int q = q0 + k * T + t;
-                    g[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (q >= inner && q < outer) g[k] = G::load4(c.grad, q);
-                }
-#pragma unroll
-                for (int k = 0; k < kN; ++k) {
-                    const double x = g[k].x, y = g[k].y, z = g[k].z, w = g[k].w;
-                    s[0] = fma(x, x, s[0]);
-                    s[1] = fma(y, y, s[1]);
-                    s[2] = fma(z, z, s[2]);
-                    s[3] = fma(w, w, s[3]);
-                }
-            }
-        }
-        for_elements<T>(c, t, [](int) {}, [&](int i) {
+                for (int i = 0; i < 4; ++i) s[i] = fma((double)x[i], (double)x[i], s[i]);
+            });
+        for_edges<T>(c, t, [&](int i) {
             const double x = G::load(c.grad, i);
             s[0] = fma(x, x, s[0]);
         });
     });
     return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// Runs body(chunk) over chunks k, k + step, ..; the next one's record is on its
+// way during a chunk.
+template <typename Body>
+__device__ __forceinline__ void for_chunks(const Chunk *chunks, int64_t n, int64_t k, int64_t step,
+                                           Body body) {
+    if (k >= n) return;
+    Chunk c = chunks[k];
+    while (true) {
+        k += step;
+        const Chunk next = chunks[k < n ? k : 0];
+        body(c);
+        if (k >= n) return;
+        c = next;
+    }
 }
 
 __device__ __forceinline__ double power(double b, int64_t t) {
@@ -245,8 +296,8 @@ __global__ __launch_bounds__(kThreads) void square_sums(Scratch *scratch, const 
                                                         int64_t n, const int64_t *step,
                                                         double beta1, double beta2) {
     double s = 0.0;
-    for (int64_t k = blockIdx.x; k < n; k += gridDim.x)
-        s += chunk_squares<kThreads>(chunks[k], threadIdx.x);
+    for_chunks(chunks, n, blockIdx.x, gridDim.x,
+               [&](const Chunk &c) { s += chunk_squares<kThreads>(c, threadIdx.x); });
     s = block_sum<kThreads>(s);
     if (threadIdx.x == 0) scratch->sums[blockIdx.x] = s;
     if (step && blockIdx.x == 0 && threadIdx.x == 0) {
@@ -276,31 +327,38 @@ __global__ __launch_bounds__(kThreads) void write_norm(const Scratch *scratch, i
 
 // --- clipping ----------------------------------------------------------------
 
-template <int T> __device__ __forceinline__ void clip_chunk(const Chunk &c, int t, float f) {
-    with_type(c.grad_dtype, [&](auto gt) {
-        with_type(c.clipped_dtype, [&](auto ct) {
+template <int T, bool STREAM>
+__device__ __forceinline__ void clip_chunk(const Chunk &c, int t, float f) {
+    if (c.clipped == c.grad && f == 1.0f) return;
+    constexpr int kN = kParamChunk / 4 / T < 8 ? kParamChunk / 4 / T : 8;
+    with_type(c.grad_dtype(), [&](auto gt) {
+        with_type(c.clipped_dtype(), [&](auto ct) {
             using G = Array<decltype(gt)::value>;
             using O = Array<decltype(ct)::value>;
-            for_elements<T>(
-                c, t,
-                [&](int q) {
-                    const float4 g = G::load4(c.grad, q);
-                    const float x[4] = {g.x * f, g.y * f, g.z * f, g.w * f};
-                    O::store4(c.clipped, q, x);
-                },
-                [&](int i) { O::store(c.clipped, i, G::load(c.grad, i) * f); });
+            typename G::Raw g[kN];
+            for_groups<T, kN>(
+                c, t, [&](int k, int q) { g[k] = get<typename G::Raw, STREAM>(c.grad, q); },
+                [&](int k, int q) {
+                    float x[4];
+                    G::unpack(g[k], x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] *= f;
+                    put<STREAM>(c.clipped, q, O::pack(x));
+                });
+            for_edges<T>(c, t, [&](int i) { O::store(c.clipped, i, G::load(c.grad, i) * f); });
         });
     });
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void clip(const Scratch *scratch, int sums,
                                                  const Chunk *chunks, int64_t n, double scale,
                                                  double max_norm, float *norm) {
     const double len = norm_of(scratch, sums, scale);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)len;
     const float f = clip_factor(len, scale, max_norm);
-    for (int64_t k = blockIdx.x; k < n; k += gridDim.x)
-        clip_chunk<kThreads>(chunks[k], threadIdx.x, f);
+    for_chunks(chunks, n, blockIdx.x, gridDim.x,
+               [&](const Chunk &c) { clip_chunk<kThreads, STREAM>(c, threadIdx.x, f); });
 }
 
 // --- update ------------------------------------------------------------------
@@ -319,43 +377,69 @@ __device__ __forceinline__ void update(const UpdateArgs &u, float corr1, float c
     p = p - u.lr * d;
 }
 
-template <int T>
-__device__ __forceinline__ void update_chunk(const Chunk &c, int t, const UpdateArgs &u, float f,
-                                             float corr1, float corr2) {
-    with_type(c.grad_dtype, [&](auto gt) {
-        using G = Array<decltype(gt)::value>;
-        using F = Array<OCTNCA_F32>;
-        for_elements<T>(
-            c, t,
-            [&](int q) {
-                const float4 g4 = G::load4(c.grad, q), p4 = F::load4(c.param, q),
-                             m4 = F::load4(c.m, q), v4 = F::load4(c.v, q);
-                float4 e4 = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (c.ema) e4 = F::load4(c.ema, q);
-                const float g[4] = {g4.x, g4.y, g4.z, g4.w};
-                float p[4] = {p4.x, p4.y, p4.z, p4.w}, m[4] = {m4.x, m4.y, m4.z, m4.w};
-                float v[4] = {v4.x, v4.y, v4.z, v4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
+// A group of four elements of an update.
+template <int DT, bool STREAM> struct Group {
+    typename Array<DT>::Raw g;
+    Words4 p, m, v, e;
+
+    __device__ __forceinline__ void load(const Chunk &c, int q) {
+        g = get<typename Array<DT>::Raw, STREAM>(c.grad, q);
+        p = get<Words4, STREAM>(c.param, q);
+        m = get<Words4, STREAM>(c.m, q);
+        v = get<Words4, STREAM>(c.v, q);
+        if (c.ema) e = get<Words4, STREAM>(c.ema, q);
+    }
+
+    __device__ __forceinline__ void finish(const Chunk &c, int q, const UpdateArgs &u, float f,
+                                           float corr1, float corr2) {
+        float gs[4], ps[4], ms[4], vs[4];
+        Array<DT>::unpack(g, gs);
+        F32::unpack(p, ps);
+        F32::unpack(m, ms);
+        F32::unpack(v, vs);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    update(u, corr1, corr2, g[k] * f, p[k], m[k], v[k]);
-                    e[k] = u.ema * e[k] + u.ema_rest * p[k];
-                }
-                F::store4(c.m, q, m);
-                F::store4(c.v, q, v);
-                F::store4(c.param, q, p);
-                if (c.ema) F::store4(c.ema, q, e);
-            },
-            [&](int i) {
-                float p = c.param[i], m = c.m[i], v = c.v[i];
-                update(u, corr1, corr2, G::load(c.grad, i) * f, p, m, v);
-                c.m[i] = m;
-                c.v[i] = v;
-                c.param[i] = p;
-                if (c.ema) c.ema[i] = u.ema * c.ema[i] + u.ema_rest * p;
-            });
+        for (int k = 0; k < 4; ++k) update(u, corr1, corr2, gs[k] * f, ps[k], ms[k], vs[k]);
+        put<STREAM>(c.m, q, F32::pack(ms));
+        put<STREAM>(c.v, q, F32::pack(vs));
+        put<STREAM>(c.param, q, F32::pack(ps));
+        if (c.ema) {
+            float es[4];
+            F32::unpack(e, es);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) es[k] = u.ema * es[k] + u.ema_rest * ps[k];
+            put<STREAM>(c.ema, q, F32::pack(es));
+        }
+    }
+};
+
+template <int T, int DT>
+__device__ __forceinline__ void update_edges(const Chunk &c, int t, const UpdateArgs &u, float f,
+                                             float corr1, float corr2) {
+    for_edges<T>(c, t, [&](int i) {
+        float p = F32::load(c.param, i), m = F32::load(c.m, i), v = F32::load(c.v, i);
+        update(u, corr1, corr2, Array<DT>::load(c.grad, i) * f, p, m, v);
+        F32::store(c.m, i, m);
+        F32::store(c.v, i, v);
+        F32::store(c.param, i, p);
+        if (c.ema) F32::store(c.ema, i, u.ema * F32::load(c.ema, i) + u.ema_rest * p);
     });
 }
 
+template <int T, bool STREAM>
+__device__ __forceinline__ void update_chunk(const Chunk &c, int t, const UpdateArgs &u, float f,
+                                             float corr1, float corr2) {
+    constexpr int kN = 2;
+    with_type(c.grad_dtype(), [&](auto gt) {
+        constexpr int DT = decltype(gt)::value;
+        Group<DT, STREAM> r[kN];
+        for_groups<T, kN>(
+            c, t, [&](int k, int q) { r[k].load(c, q); },
+            [&](int k, int q) { r[k].finish(c, q, u, f, corr1, corr2); });
+        update_edges<T, DT>(c, t, u, f, corr1, corr2);
+    });
+}
+
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void adamw(const Scratch *scratch, int sums,
                                                   const Chunk *chunks, int64_t n, UpdateArgs u,
                                                   int64_t *step, float *norm) {
@@ -366,9 +450,91 @@ __global__ __launch_bounds__(kThreads) void adamw(const Scratch *scratch, int su
     if (first) *step += 1;
     const float f = clip_factor(len, u.scale, u.max_norm);
     const float corr1 = (float)scratch->corr1, corr2 = (float)scratch->corr2;
-    for (int64_t k = blockIdx.x; k < n; k += gridDim.x)
-        update_chunk<kThreads>(chunks[k], threadIdx.x, u, f, corr1, corr2);
+    for_chunks(chunks, n, blockIdx.x, gridDim.x, [&](const Chunk &c) {
+        update_chunk<kThreads, STREAM>(c, threadIdx.x, u, f, corr1, corr2);
+    });
 }
+
+// --- small lists: one launch --------------------------------------------------
+
+// A small list takes one launch: every workgroup sums all gradients itself (in
+// the same order), then does one chunk.  The sum of 16.5k elements costs a
+// workgroup less than a second launch would.
+constexpr int kSmallThreads = 1024;
+
+// scale * norm of the list; wave w of the workgroup takes chunks w, w + 16, ..
+__device__ __forceinline__ double small_norm(const Chunk *chunks, int n, double scale) {
+    double s = 0.0;
+    for_chunks(chunks, n, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kSmallThreads / 64,
+               [&](const Chunk &c) { s += chunk_squares<64>(c, threadIdx.x & 63); });
+    return sqrt(block_sum<kSmallThreads>(s)) * scale;
+}
+
+__global__ __launch_bounds__(kSmallThreads) void small_write_norm(const Chunk *chunks, int n,
+                                                                  double scale, float *norm) {
+    const double len = small_norm(chunks, n, scale);
+    if (threadIdx.x == 0) *norm = (float)len;
+}
+
+// Not in place: another workgroup may still be summing.
+__global__ __launch_bounds__(kSmallThreads) void small_clip(const Chunk *chunks, int n,
+                                                            double scale, double max_norm,
+                                                            float *norm) {
+    const double len = small_norm(chunks, n, scale);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)len;
+    if (n == 0) return;
+    clip_chunk<kSmallThreads, false>(chunks[blockIdx.x], threadIdx.x,
+                                     clip_factor(len, scale, max_norm));
+}
+
+// The workgroup's own chunk is read before the sum, so that both wait together.
+__global__ __launch_bounds__(kSmallThreads) void small_adamw(Scratch *scratch, const Chunk *chunks,
+                                                             int n, UpdateArgs u, double beta1,
+                                                             double beta2, int64_t *step,
+                                                             float *norm) {
+    static_assert(kParamChunk / 4 == kSmallThreads, "one group of four a thread");
+    const int64_t t = __hip_atomic_load(step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    Chunk c{};
+    if (n > 0) c = chunks[blockIdx.x];
+    with_type(c.grad_dtype(), [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        const int q = threadIdx.x;
+        const bool whole = c.quads && q >= (c.first + 3) / 4 && q < c.end / 4;
+        Group<DT, false> own;
+        if (whole) own.load(c, q);
+        const double len = small_norm(chunks, n, u.scale);
+        const bool fine = __builtin_isfinite(len);
+        if (threadIdx.x == 0) {
+            if (norm && blockIdx.x == 0) *norm = (float)len;
+            // The workgroup that counts last writes *step: the others have read
+            // it before they counted (acq_rel).
+            const uint32_t before = __hip_atomic_fetch_add(&scratch->done, 1u, __ATOMIC_ACQ_REL,
+                                                           __HIP_MEMORY_SCOPE_AGENT);
+            if (before == gridDim.x - 1) {
+                scratch->done = 0;
+                if (fine) *step = t;
+            }
+        }
+        if (n == 0 || !fine) return;
+        const float f = clip_factor(len, u.scale, u.max_norm);
+        const float corr1 = (float)(1.0 / (1.0 - power(beta1, t)));
+        const float corr2 = (float)(1.0 / (1.0 - power(beta2, t)));
+        if (whole) own.finish(c, q, u, f, corr1, corr2);
+        update_edges<kSmallThreads, DT>(c, threadIdx.x, u, f, corr1, corr2);
+    });
+}
+
+// Lists that take one launch.
+constexpr int64_t kSmallElements = 1 << 15;
+constexpr int64_t kSmallChunks = 64;
+bool small(const octnca_param_list &l) {
+    return l.elements <= kSmallElements && l.chunks <= kSmallChunks;
+}
+unsigned small_grid(const octnca_param_list &l) { return (unsigned)std::max<int64_t>(1, l.chunks); }
+
+// Lists whose arrays pass the last-level cache of 256 MB before the next call:
+// the second pass then goes past it.
+bool streams(const octnca_param_list &l) { return l.bytes >= (int64_t(1) << 27); }
 
 // Enqueues the first pass; the number of sums it leaves.
 int first_pass(const octnca_param_list &l, const int64_t *step, double beta1, double beta2,
@@ -410,6 +576,11 @@ hipError_t launch_param_table(const octnca_param *params, int n, void *table, hi
 
 hipError_t launch_grad_norm(const octnca_param_list &l, double scale, float *norm,
                             hipStream_t stream) {
+    if (small(l)) {
+        small_write_norm<<<1, kSmallThreads, 0, stream>>>(chunks_of(l.table), (int)l.chunks, scale,
+                                                          norm);
+        return hipGetLastError();
+    }
     const int sums = first_pass(l, nullptr, 0.0, 0.0, stream);
     write_norm<<<1, kThreads, 0, stream>>>(scratch_of(l.table), sums, scale, norm);
     return hipGetLastError();
@@ -417,16 +588,21 @@ hipError_t launch_grad_norm(const octnca_param_list &l, double scale, float *nor
 
 hipError_t launch_clip_grads(const octnca_param_list &l, double scale, double max_norm,
                              float *norm, hipStream_t stream) {
+    if (small(l) && !(l.has & kHasInPlace)) {
+        small_clip<<<small_grid(l), kSmallThreads, 0, stream>>>(
+            chunks_of(l.table), (int)l.chunks, scale, max_norm, norm);
+        return hipGetLastError();
+    }
     const int sums = first_pass(l, nullptr, 0.0, 0.0, stream);
-    clip<<<second_grid(l.chunks), kThreads, 0, stream>>>(scratch_of(l.table), sums,
-                                                         chunks_of(l.table), l.chunks, scale,
-                                                         max_norm, norm);
+    const auto kernel = streams(l) ? clip<true> : clip<false>;
+    kernel<<<second_grid(l.chunks), kThreads, 0, stream>>>(scratch_of(l.table), sums,
+                                                           chunks_of(l.table), l.chunks, scale,
+                                                           max_norm, norm);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64_t *step,
                         float *norm, hipStream_t stream) {
-    const int sums = first_pass(l, step, h.beta1, h.beta2, stream);
     UpdateArgs u;
     u.scale = h.scale;
     u.max_norm = h.max_norm;
@@ -439,9 +615,17 @@ hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64
     u.decay = (float)h.weight_decay;
     u.ema = (float)h.ema_decay;
     u.ema_rest = (float)(1.0 - h.ema_decay);
-    adamw<<<second_grid(l.chunks), kThreads, 0, stream>>>(scratch_of(l.table), sums,
-                                                          chunks_of(l.table), l.chunks, u, step,
-                                                          norm);
+    if (small(l)) {
+        small_adamw<<<small_grid(l), kSmallThreads, 0, stream>>>(
+            scratch_of(l.table), chunks_of(l.table), (int)l.chunks, u, h.beta1, h.beta2, step,
+            norm);
+        return hipGetLastError();
+    }
+    const int sums = first_pass(l, step, h.beta1, h.beta2, stream);
+    const auto kernel = streams(l) ? adamw<true> : adamw<false>;
+    kernel<<<second_grid(l.chunks), kThreads, 0, stream>>>(scratch_of(l.table), sums,
+                                                           chunks_of(l.table), l.chunks, u, step,
+                                                           norm);
     return hipGetLastError();
 }
 

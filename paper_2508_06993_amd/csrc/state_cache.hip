@@ -1,6 +1,7 @@
 // State cache: states in 8 bits with a scale for each block of cells and
 // channel (formulas in octree_nca.h).
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 
@@ -10,48 +11,106 @@ namespace {
 
 constexpr float kTiny = 0x1p-100f;   // the smallest magnitude that sets a scale
 
-template <typename T> struct Quad;   // four channels of a cell as stored
+typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+
+// Loads and stores that go past the last-level cache (STREAM) or through it.
+template <bool STREAM, typename R> __device__ __forceinline__ R get(const R *p) {
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool STREAM, typename R> __device__ __forceinline__ void put(R *p, R x) {
+    if (STREAM)
+        __builtin_nontemporal_store(x, p);
+    else
+        *p = x;
+}
+
+// Four channels of a cell as stored; Top keeps the largest magnitudes of four
+// channels, as bits (the order of the bits of magnitudes is that of the values,
+// with infinities and NaNs above all numbers).
+template <typename T> struct Quad;
 template <> struct Quad<float> {
-    using Raw = uint4;
-    static __device__ __forceinline__ void unpack(const Raw &v, float *x) {
-        Storage<float>::unpack(v, x);
+    using Raw = Words4;
+    static __device__ __forceinline__ void unpack(Raw v, float *x) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = __uint_as_float(v[k]);
     }
-    static __device__ __forceinline__ Raw pack(const float *x) { return Storage<float>::pack(x); }
+    static __device__ __forceinline__ Raw pack(const float *x) {
+        return Raw{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                   __float_as_uint(x[3])};
+    }
+    struct Top {
+        Words4 m = {0, 0, 0, 0};
+        __device__ __forceinline__ void add(Raw v) {
+            m = __builtin_elementwise_max(m, v & 0x7fffffffu);
+        }
+        __device__ __forceinline__ Words4 bits() const { return m; }
+    };
 };
 template <> struct Quad<__half> {
-    using Raw = uint2;
-    static __device__ __forceinline__ void unpack(const Raw &v, float *x) {
+    using Raw = Words2;
+    static __device__ __forceinline__ void unpack(Raw v, float *x) {
         Storage<__half>::unpack_pair(v.x, x[0], x[1]);
         Storage<__half>::unpack_pair(v.y, x[2], x[3]);
     }
     static __device__ __forceinline__ Raw pack(const float *x) {
-        return make_uint2(Storage<__half>::pack_pair(x[0], x[1]),
-                          Storage<__half>::pack_pair(x[2], x[3]));
+        return Raw{Storage<__half>::pack_pair(x[0], x[1]), Storage<__half>::pack_pair(x[2], x[3])};
     }
+    struct Top {
+        typedef uint16_t Halves __attribute__((ext_vector_type(4)));
+        Halves m = {0, 0, 0, 0};
+        __device__ __forceinline__ void add(Raw v) {
+            m = __builtin_elementwise_max(m, __builtin_bit_cast(Halves, v & 0x7fff7fffu));
+        }
+        // as fp32 bits
+        __device__ __forceinline__ Words4 bits() const {
+            float x[4];
+            unpack(__builtin_bit_cast(Raw, m), x);
+            return Quad<float>::pack(x);
+        }
+    };
 };
 
+constexpr uint32_t kInfBits = 0x7f800000u;
+
 // Factor and scale of a block's channel from a = max(A, 2^-100), and the codes
-// of four values (lowest byte first) and back.
+// of four values (lowest byte first) and back.  ODD: some of the values may not
+// be finite.
 struct CodeI8 {
     static __device__ __forceinline__ void scale_of(float a, float &inv, float &scale) {
         inv = 127.0f / a;
         scale = a / 127.0f;
     }
-    // a finite |x| is at most a, so |x * inv| <= 127 (1 + 2^-23) rounds to 127 at most
-    static __device__ __forceinline__ uint32_t one(float x, float inv) {
-        const int c = (int)rintf(x * inv);
-        return (uint32_t)(__builtin_isfinite(x) ? c : -128) & 0xffu;
+    // |x| is at most a, so |x * inv| <= 127 (1 + 2^-23) rounds to 127 at most.
+    // Adding 1.5 * 2^23 rounds to an integer, ties to even, and leaves it in
+    // the low bits; the product is rounded before (no fused multiply-add).
+    static __device__ __forceinline__ uint32_t nearest(float x, float inv) {
+#pragma clang fp contract(off)
+        return __float_as_uint(x * inv + 0x1.8p23f);
     }
-    static __device__ __forceinline__ uint32_t encode(const float *x, const float *inv) {
-        return one(x[0], inv[0]) | one(x[1], inv[1]) << 8 | one(x[2], inv[2]) << 16 |
-               one(x[3], inv[3]) << 24;
-    }
-    static __device__ __forceinline__ void decode(uint32_t c, const float *scale, float *x) {
+    template <bool ODD> static __device__ __forceinline__ uint32_t encode(const float *x,
+                                                                          const float *inv) {
+        uint32_t c[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int v = (int)(int8_t)(c >> (8 * k));
-            x[k] = v == -128 ? __builtin_nanf("") : (float)v * scale[k];
+            c[k] = nearest(x[k], inv[k]);
+            if (ODD && !__builtin_isfinite(x[k])) c[k] = 0x80u;
         }
+        // the low bytes of the four, in order
+        return __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u) |
+               __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);
+    }
+    // With the sign bit flipped a byte is code + 128, which has a conversion of
+    // its own for each byte.
+    static __device__ __forceinline__ void decode(uint32_t c, const float *scale, float *x) {
+        const uint32_t u = c ^ 0x80808080u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            x[k] = ((float)(u >> (8 * k) & 0xffu) - 128.0f) * scale[k];
+        if ((u - 0x01010101u) & ~u & 0x80808080u)   // a byte is 0: code -128
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if ((u >> (8 * k) & 0xffu) == 0) x[k] = __builtin_nanf("");
     }
 };
 
@@ -64,12 +123,13 @@ struct CodeF8 {
         scale = __uint_as_float((e - 8) << 23);
         inv = __uint_as_float((262 - e) << 23);
     }
-    static __device__ __forceinline__ uint32_t encode(const float *x, const float *inv) {
+    template <bool ODD> static __device__ __forceinline__ uint32_t encode(const float *x,
+                                                                          const float *inv) {
         float y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            y[k] = __builtin_isfinite(x[k]) ? x[k] * inv[k] : __builtin_nanf("");
-        int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            y[k] = !ODD || __builtin_isfinite(x[k]) ? x[k] * inv[k] : __builtin_nanf("");
+        const int c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
     }
     static __device__ __forceinline__ void decode(uint32_t c, const float *scale, float *x) {
@@ -83,7 +143,7 @@ struct CodeF8 {
 constexpr int kWaves = 4;              // per workgroup, each with blocks of its own
 constexpr int64_t kMaxGrid = 1 << 20;  // workgroups along x; the kernels loop over the rest
 
-// Work split of both kernels: a wave takes one block of cells (of one state),
+// Work split of the writes: a wave takes whole blocks of cells of one state,
 // whose channel quads lie one after the other in memory.  Lane l takes quads l,
 // l + kLanes, ..: kLanes is a multiple of the quads per cell, so a lane stays
 // with one channel quad, and a pass of the wave is contiguous in memory.
@@ -103,36 +163,38 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 // Largest of the 16 lanes of a row, in every lane: rotations by 1, 2, 4, 8.
-__device__ __forceinline__ float row_max(float x) {
-    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x121, 15, 15, true)));
-    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x122, 15, 15, true)));
-    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x124, 15, 15, true)));
-    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 15, 15, true)));
-    return x;
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+    x = std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 15, 15, true));
+    x = std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 15, 15, true));
+    x = std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 15, 15, true));
+    return std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 15, 15, true));
 }
 
-// Largest values (4 channels a lane) over the lanes of one channel quad, in
-// each of them: every lane leaves its four in LDS by quad, row r of 16 lanes
-// reduces quads r, r + 4, .., and each lane fetches its quad's.
-template <int Q, int PEERS>
-__device__ __forceinline__ void quad_max(float (*peers)[4], float (*top)[4], float *m) {
+// Largest magnitudes of the channels of N blocks, tops[block][channel], from
+// those of each lane's channel quad: every lane leaves its four in LDS by quad,
+// and row r of 16 lanes reduces quads r, r + 4, ..
+template <int Q, int PEERS, int N>
+__device__ __forceinline__ void quad_max(Words4 (*peers)[64], Words4 (*tops)[Q], const Words4 *m) {
     const int lane = threadIdx.x & 63;
     if (lane < Q * PEERS)
-        *(float4 *)peers[lane % Q * PEERS + lane / Q] = make_float4(m[0], m[1], m[2], m[3]);
+#pragma unroll
+        for (int b = 0; b < N; ++b) peers[b][lane % Q * PEERS + lane / Q] = m[b];
     wave_fence();
     for (int q = lane >> 4; q < Q; q += 4) {
-        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = lane & 15; k < PEERS; k += 16) {
-            const float4 v = *(const float4 *)peers[q * PEERS + k];
-            t = make_float4(fmaxf(t.x, v.x), fmaxf(t.y, v.y), fmaxf(t.z, v.z), fmaxf(t.w, v.w));
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            Words4 t = {0, 0, 0, 0};
+#pragma unroll
+            for (int k0 = 0; k0 < PEERS; k0 += 16) {
+                const int k = k0 + (lane & 15);
+                if (k < PEERS) t = __builtin_elementwise_max(t, peers[b][q * PEERS + k]);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) t[c] = row_max(t[c]);
+            if ((lane & 15) == 0) tops[b][q] = t;
         }
-        t = make_float4(row_max(t.x), row_max(t.y), row_max(t.z), row_max(t.w));
-        if ((lane & 15) == 0) *(float4 *)top[q] = t;
     }
     wave_fence();
-    const float4 t = *(const float4 *)top[lane % Q];
-    m[0] = t.x, m[1] = t.y, m[2] = t.z, m[3] = t.w;
-    wave_fence();   // the next block's maxima come after these reads
 }
 
 // Slot of state i; whether it is one of the cache's.
@@ -149,124 +211,222 @@ __device__ __forceinline__ bool written_later(const CacheArgs &a, int i, int64_t
     return __any(found);
 }
 
-// The block's values stay in registers between the maxima and the codes.
-template <typename T, int C, int B, typename Code>
-__global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a,
-                                                           const T *__restrict__ states) {
+// Calls f with `flag` as a constant.
+template <typename F> __device__ __forceinline__ void with_flag(bool flag, F f) {
+    if (flag)
+        f(std::true_type());
+    else
+        f(std::false_type());
+}
+
+// Loads, maxima, factors and codes of N consecutive blocks of a state (cells of
+// them, src: their first) by one wave; FULL: cells = N B.  LDS of the wave:
+// peers, tops.
+template <typename T, int C, int B, int N, typename Code, bool FULL, bool STREAM>
+__device__ __forceinline__ void write_blocks(const CacheArgs &a, int i, int64_t cell, int cells,
+                                             const T *src_cells, Words4 (*peers)[64],
+                                             Words4 (*tops)[C / 4]) {
     using S = Split<C, B>;
     using Raw = typename Quad<T>::Raw;
-    __shared__ __align__(16) float peers[kWaves][64][4];
-    __shared__ __align__(16) float tops[kWaves][S::kQ][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t blocks = (a.count + B - 1) / B;
-    for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
-        const T *from = states + (int64_t)i * a.count * C;
-        for (int64_t b = (int64_t)blockIdx.x * kWaves + wave; b < blocks;
-             b += (int64_t)gridDim.x * kWaves) {
-            const int64_t left = a.count - b * B;
-            const int quads = lane < S::kLanes ? (int)(left < B ? left : B) * S::kQ : 0;
-            const Raw *src = (const Raw *)(from + b * B * C);
-            float x[S::kPasses][4];
-            float m[4] = {kTiny, kTiny, kTiny, kTiny};
+    const int lane = threadIdx.x & 63;
+    const Raw *src = (const Raw *)src_cells;
+    // whether the lane has a quad in pass k of block b
+    const auto has = [&](int b, int k) {
+        const int q = lane + k * S::kLanes;
+        const bool in = lane < S::kLanes && ((k + 1) * S::kLanes <= B * S::kQ || q < B * S::kQ);
+        return FULL ? in : in && q < (cells - b * B) * S::kQ;
+    };
+    // where it has none, it loads its channels of the block's first cell (of
+    // the first block's, if the block is past the end) once more: no branches,
+    // and the maxima stay what they are
+    Raw raw[N][S::kPasses];
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int k = 0; k < S::kPasses; ++k) {
+            const int at = FULL || b * B < cells ? b * B * S::kQ : 0;
+            raw[b][k] = get<STREAM>(src + (has(b, k) ? b * B * S::kQ + k * S::kLanes + lane
+                                                     : at + lane % S::kQ));
+        }
+    Words4 m[N];
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+        typename Quad<T>::Top top;
+#pragma unroll
+        for (int k = 0; k < S::kPasses; ++k) top.add(raw[b][k]);
+        m[b] = top.bits();
+    }
+    quad_max<S::kQ, S::kPeers, N>(peers, tops, m);
+    // the slot is looked up behind the loads, which do not need it
+    int64_t slot;
+    if (!slot_of(a, i, slot) || written_later(a, i, slot)) return;
+    float *scales = a.scales + (slot * a.blocks + (a.from + cell) / B) * C;
+    // one lane a channel and block: its factor takes its maximum's place
+    uint32_t *values = (uint32_t *)tops;
+    bool odd = false;
+    for (int e = lane; e < N * C; e += 64) odd |= values[e] >= kInfBits;
+    odd = __any(odd);
+    if (odd) {   // again over the finite values
+        wave_fence();
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            m[b] = Words4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < S::kPasses; ++k) {
-                const int q = lane + k * S::kLanes;
-                Raw r{};
-                if (q < quads) r = src[q];
-                Quad<T>::unpack(r, x[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < S::kPasses; ++k)
+                float x[4];
+                Quad<T>::unpack(raw[b][k], x);
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
-                    m[c] = fmaxf(m[c], __builtin_isfinite(x[k][c]) ? fabsf(x[k][c]) : 0.f);
-            quad_max<S::kQ, S::kPeers>(peers[wave], tops[wave], m);
-            // the slot is looked up behind the block's loads, which do not need it
-            int64_t slot;
-            if (!slot_of(a, i, slot) || written_later(a, i, slot)) break;
-            int8_t *codes = a.codes + (slot * a.cells + a.from) * C;
-            float *scales = a.scales + (slot * a.blocks + a.from / B) * C;
-            float inv[4], scale[4];
+                    if (__builtin_isfinite(x[c]))
+                        m[b][c] = std::max(m[b][c], __float_as_uint(fabsf(x[c])));
+            }
+        }
+        quad_max<S::kQ, S::kPeers, N>(peers, tops, m);
+    }
+    for (int e = lane; e < N * C; e += 64) {
+        float inv, scale;
+        Code::scale_of(fmaxf(__uint_as_float(values[e]), kTiny), inv, scale);
+        if (FULL || e / C * B < cells) scales[e] = scale;
+        values[e] = __float_as_uint(inv);
+    }
+    wave_fence();
+    uint32_t *dst = (uint32_t *)(a.codes + (slot * a.cells + a.from + cell) * C);
+    with_flag(odd, [&](auto is_odd) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) Code::scale_of(m[c], inv[c], scale[c]);
-            uint32_t *dst = (uint32_t *)(codes + b * B * C);
+        for (int b = 0; b < N; ++b) {
+            float inv[4];
+            Quad<float>::unpack(tops[b][lane % S::kQ], inv);
 #pragma unroll
             for (int k = 0; k < S::kPasses; ++k) {
-                const int q = lane + k * S::kLanes;
-                if (q < quads) dst[q] = Code::encode(x[k], inv);
+                float x[4];
+                Quad<T>::unpack(raw[b][k], x);
+                const uint32_t c = Code::template encode<decltype(is_odd)::value>(x, inv);
+                if (has(b, k)) put<STREAM>(dst + b * B * S::kQ + k * S::kLanes + lane, c);
             }
-            if (lane < S::kQ)
-                ((float4 *)(scales + b * C))[lane] =
-                    make_float4(scale[0], scale[1], scale[2], scale[3]);
+        }
+    });
+    wave_fence();   // the next maxima come after these reads
+}
+
+// A wave takes N consecutive blocks at a time, with all their loads in flight.
+// The values stay in registers between the maxima and the codes.
+template <typename T, int C, int B, int N, typename Code>
+__global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a,
+                                                           const T *__restrict__ states) {
+    __shared__ Words4 peers[kWaves][N][64];
+    __shared__ Words4 tops[kWaves][N][C / 4];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
+        const T *from = states + (int64_t)i * a.count * C;
+        for (int64_t g = (int64_t)blockIdx.x * kWaves + wave; g * N * B < a.count;
+             g += (int64_t)gridDim.x * kWaves) {
+            const int64_t cell = g * N * B;
+            const int cells = (int)std::min<int64_t>(a.count - cell, N * B);
+            if (cells == N * B)
+                with_flag(a.stream, [&](auto stream) {
+                    write_blocks<T, C, B, N, Code, true, decltype(stream)::value>(
+                        a, i, cell, cells, from + cell * C, peers[wave], tops[wave]);
+                });
+            else
+                write_blocks<T, C, B, N, Code, false, false>(a, i, cell, cells, from + cell * C,
+                                                             peers[wave], tops[wave]);
         }
     }
 }
 
-template <typename T, int C, int B, typename Code>
-__global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, T *__restrict__ states) {
-    using S = Split<C, B>;
+// A thread takes channel quads of a state, the workgroup's threads apart: 32
+// bytes of the state's values.
+template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
+template <typename T, int C, typename Code>
+__global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift,
+                                                          T *__restrict__ states) {
+    constexpr int kQ = C / 4, kThreads = 64 * kWaves, kN = kReadQuads<T>;
     using Raw = typename Quad<T>::Raw;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t blocks = (a.count + B - 1) / B;
+    const int64_t quads = a.count * kQ;
     for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
         int64_t slot;
         const bool there = slot_of(a, i, slot);
-        T *to = states + (int64_t)i * a.count * C;
-        const int8_t *codes = a.codes + (slot * a.cells + a.from) * C;
-        const float *scales = a.scales + (slot * a.blocks + a.from / B) * C;
-        for (int64_t b = (int64_t)blockIdx.x * kWaves + wave; b < blocks;
-             b += (int64_t)gridDim.x * kWaves) {
-            const int64_t left = a.count - b * B;
-            const int quads = lane < S::kLanes ? (int)(left < B ? left : B) * S::kQ : 0;
-            uint32_t code[S::kPasses] = {};
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (there) {
-                const uint32_t *src = (const uint32_t *)(codes + b * B * C);
-                s = ((const float4 *)(scales + b * C))[lane % S::kQ];
+        Raw *to = (Raw *)(states + (int64_t)i * a.count * C);
+        const uint32_t *codes = (const uint32_t *)(a.codes + (slot * a.cells + a.from) * C);
+        const float4 *scales = (const float4 *)(a.scales + (slot * a.blocks + (a.from >> shift)) * C);
+        for (int64_t base = (int64_t)blockIdx.x * kN * kThreads; base < quads;
+             base += (int64_t)gridDim.x * kN * kThreads) {
+            const int left = (int)std::min<int64_t>(quads - base, kN * kThreads);
+            const int64_t cell = base / kQ;                 // of the first quad, and its place in it
+            const int over = (int)(base - cell * kQ);
+            uint32_t code[kN] = {};
+            float4 s[kN] = {};
+            if (there)
+                with_flag(a.stream, [&](auto stream) {
 #pragma unroll
-                for (int k = 0; k < S::kPasses; ++k) {
-                    const int q = lane + k * S::kLanes;
-                    if (q < quads) code[k] = src[q];
+                    for (int k = 0; k < kN; ++k) {
+                        const int q = threadIdx.x + k * kThreads;
+                        if (q >= left) continue;
+                        code[k] = get<decltype(stream)::value>(codes + base + q);
+                        const int c = (q + over) / kQ;
+                        s[k] = scales[((cell + c) >> shift) * kQ + (q + over - c * kQ)];
+                    }
+                });
+            with_flag(a.stream, [&](auto stream) {
+#pragma unroll
+                for (int k = 0; k < kN; ++k) {
+                    const int q = threadIdx.x + k * kThreads;
+                    const float scale[4] = {s[k].x, s[k].y, s[k].z, s[k].w};
+                    float x[4];
+                    Code::decode(code[k], scale, x);
+                    if (q < left) put<decltype(stream)::value>(to + base + q, Quad<T>::pack(x));
                 }
-            }
-            const float scale[4] = {s.x, s.y, s.z, s.w};
-            Raw *dst = (Raw *)(to + b * B * C);
-#pragma unroll
-            for (int k = 0; k < S::kPasses; ++k) {
-                const int q = lane + k * S::kLanes;
-                float x[4];
-                Code::decode(code[k], scale, x);
-                if (q < quads) dst[q] = Quad<T>::pack(x);
-            }
+            });
         }
     }
 }
 
-template <typename T, int C, int B, typename Code>
-hipError_t run(const CacheArgs &a, bool write, void *states, hipStream_t stream) {
-    const int64_t groups = ((a.count + B - 1) / B + kWaves - 1) / kWaves;
+template <typename T, int C, int B, int N, typename Code>
+hipError_t launch_write(const CacheArgs &a, const void *states, hipStream_t stream) {
+    const int64_t groups = (a.count + (int64_t)B * N * kWaves - 1) / (B * N * kWaves);
     const dim3 grid((unsigned)std::min(groups, kMaxGrid), (unsigned)std::min(a.n, 65535));
-    if (write)
-        cache_write<T, C, B, Code><<<grid, 64 * kWaves, 0, stream>>>(a, (const T *)states);
-    else
-        cache_read<T, C, B, Code><<<grid, 64 * kWaves, 0, stream>>>(a, (T *)states);
+    cache_write<T, C, B, N, Code><<<grid, 64 * kWaves, 0, stream>>>(a, (const T *)states);
     return hipGetLastError();
 }
 
+// Blocks a wave takes at a time: as many as make a lane's loads in flight about
+// 64 bytes (32 for fp16: 128 cells), where even so every SIMD gets several
+// waves; else one, for the most waves.  Four 2048 x 2048 states (1 GB) with 32
+// cells a block, one block and this many: C = 12 fp32 4.2 and 5.5 TB/s, C = 16
+// 5.9 and 6.1; fp16 2.7 and 5.0, 4.4 and 5.9.
+template <typename T, int C, int B, typename Code>
+hipError_t run_write(const CacheArgs &a, const void *states, hipStream_t stream) {
+    constexpr int kCells = sizeof(T) == 4 ? 64 : 128;
+    if (B < kCells && a.count * a.n >= int64_t(kCells) * 8192)
+        return launch_write<T, C, B, (B < kCells ? kCells / B : 1), Code>(a, states, stream);
+    return launch_write<T, C, B, 1, Code>(a, states, stream);
+}
+
 template <typename T, int C, typename Code>
-hipError_t run_block(const CacheArgs &a, bool write, void *states, hipStream_t stream) {
+hipError_t run(CacheArgs a, bool write, void *states, hipStream_t stream) {
+    // past this size nothing of the call is still in the last-level cache (256 MB)
+    // when it is wanted next
+    a.stream = a.count * a.n * C * (int64_t)(sizeof(T) + 1) >= int64_t(1) << 27;
+    if (!write) {
+        const int64_t per = kReadQuads<T> * 64 * kWaves;
+        const int64_t groups = (a.count * (C / 4) + per - 1) / per;
+        const dim3 grid((unsigned)std::min(groups, kMaxGrid), (unsigned)std::min(a.n, 65535));
+        const int shift = a.block == 32 ? 5 : a.block == 64 ? 6 : 7;
+        cache_read<T, C, Code><<<grid, 64 * kWaves, 0, stream>>>(a, shift, (T *)states);
+        return hipGetLastError();
+    }
     switch (a.block) {
-        case 32: return run<T, C, 32, Code>(a, write, states, stream);
-        case 64: return run<T, C, 64, Code>(a, write, states, stream);
-        case 128: return run<T, C, 128, Code>(a, write, states, stream);
+        case 32: return run_write<T, C, 32, Code>(a, states, stream);
+        case 64: return run_write<T, C, 64, Code>(a, states, stream);
+        case 128: return run_write<T, C, 128, Code>(a, states, stream);
     }
     return hipErrorInvalidValue;
 }
 
 template <typename T, int C>
 hipError_t run_code(const CacheArgs &a, bool write, void *states, hipStream_t stream) {
-    return a.f8 ? run_block<T, C, CodeF8>(a, write, states, stream)
-                : run_block<T, C, CodeI8>(a, write, states, stream);
+    return a.f8 ? run<T, C, CodeF8>(a, write, states, stream)
+                : run<T, C, CodeI8>(a, write, states, stream);
 }
 
 template <typename T>
