@@ -475,6 +475,32 @@ int octree_nca_state_cache_read(const octnca_model *model, const octnca_state_ca
                                 void *states, int64_t from, int64_t count, int32_t n,
                                 const int64_t *slots, int64_t first, void *stream);
 
+/* How a training step keeps its states. */
+typedef struct {
+    int32_t code;   /* octnca_code */
+    int32_t block;  /* cells that share a scale: 32, 64 or 128 */
+} octnca_keep;
+
+/* Bytes of workspace octree_nca_train_step_kept needs (0 if an argument is
+ * invalid): pyramid images, every state of every level in 8 bits, four
+ * finest-size states, two finest-size gradients and the backward's workspace. */
+size_t octree_nca_train_kept_workspace_bytes(const octnca_model *model, octnca_extent finest,
+                                             int32_t levels, const int32_t *factors,
+                                             const int32_t *steps, const octnca_keep *keep);
+
+/* octree_nca_train_step with the states before each step kept in a state cache
+ * (as octree_nca_state_cache_write would): the forward, its final state and the
+ * loss are those of octree_nca_train_step; the backward takes each step at the
+ * state that reads back, so the gradients carry the codes' rounding.  workspace
+ * is 16-byte aligned.  Errors as octree_nca_train_step. */
+int octree_nca_train_step_kept(const octnca_model *model, const void *image, octnca_extent finest,
+                               int32_t levels, const int32_t *factors,
+                               const octnca_level_weights *weights, const int32_t *steps,
+                               float fire_rate, uint64_t seed, const float *target,
+                               const octnca_keep *keep, void *workspace, size_t workspace_bytes,
+                               const octnca_level_grads *grads, double *loss, void *final_state,
+                               void *stream);
+
 /* ---------------------------------------------------------------------------
  * Gradients of many tensors: their global norm, clipping by it, and the
  * clipped AdamW update (the paper trains with Adam and a running average of

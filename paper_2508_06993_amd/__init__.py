@@ -33,7 +33,8 @@ __all__ = [
     "level_grads_struct", "StateCacheBuffers", "state_cache_refs", "octree_nca_state_cache_write",
     "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
     "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
-    "octree_nca_adamw", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
+    "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
+    "octree_nca_train_step_kept", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
     "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
     "OCTNCA_EUNSUPPORTED", "OCTNCA_ESHAPE",
     "OCTNCA_EHIP", "OCTNCA_ESPACE", "OCTNCA_F32", "OCTNCA_F16", "KERNEL_NAMES", "kernel_fields",
@@ -86,7 +87,8 @@ EXPORTED_SYMBOLS = (
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
     "octree_nca_state_cache_write", "octree_nca_state_cache_read",
     "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm",
-    "octree_nca_clip_grads", "octree_nca_adamw",
+    "octree_nca_clip_grads", "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
+    "octree_nca_train_step_kept",
 )
 
 
@@ -121,6 +123,10 @@ class _StateCache(ctypes.Structure):
     _fields_ = [("code", ctypes.c_int32), ("block", ctypes.c_int32), ("slots", ctypes.c_int64),
                 ("cells", ctypes.c_int64), ("codes", ctypes.c_void_p),
                 ("scales", ctypes.c_void_p)]
+
+
+class _Keep(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_int32), ("block", ctypes.c_int32)]
 
 
 class _Param(ctypes.Structure):
@@ -197,6 +203,15 @@ _SIGS = {
                                             _P, _I64, _I64, _I32, _P, _I64, _P]),
     "octree_nca_state_cache_read": (_I32, [ctypes.POINTER(_Model), ctypes.POINTER(_StateCache),
                                            _P, _I64, _I64, _I32, _P, _I64, _P]),
+    "octree_nca_train_kept_workspace_bytes": (ctypes.c_size_t,
+                                              [ctypes.POINTER(_Model), _Extent, _I32,
+                                               ctypes.POINTER(_I32), ctypes.POINTER(_I32),
+                                               ctypes.POINTER(_Keep)]),
+    "octree_nca_train_step_kept": (_I32, [ctypes.POINTER(_Model), _P, _Extent, _I32,
+                                          ctypes.POINTER(_I32), ctypes.POINTER(_LevelWeights),
+                                          ctypes.POINTER(_I32), ctypes.c_float, ctypes.c_uint64,
+                                          _P, ctypes.POINTER(_Keep), _P, ctypes.c_size_t,
+                                          ctypes.POINTER(_LevelGrads), _P, _P, _P]),
     "octree_nca_param_table_bytes": (ctypes.c_size_t, [ctypes.POINTER(_Param), _I32]),
     "octree_nca_param_table": (_I32, [ctypes.POINTER(_Param), _I32, _P, ctypes.c_size_t,
                                       ctypes.POINTER(_ParamList), _P]),
@@ -263,27 +278,28 @@ def _extent(ext: Sequence[int]) -> _Extent:
 
 
 def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
+    """Address of a contiguous device tensor (an int; None for None)."""
     if t is None:
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
     if not t.is_contiguous():
         raise OctreeNCAError(f"{name}: must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise OctreeNCAError(f"{name}: expected {dtype}, got {t.dtype}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int:
     if stream is None:
         # the current stream's handle; torch.cuda.current_stream() would also
         # make a Stream object, 2.7 us a call
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
 def _factors(factors: Sequence[Sequence[int]]):
@@ -600,11 +616,11 @@ def _cache_call(name, model, refs, states, from_cell, slots, first, stream):
     n, c = shape[0], shape[-1]
     if c != model.channels:
         raise OctreeNCAError(f"states: expected {model.channels} channels, got {c}")
-    if slots is not None and tuple(slots.shape) != (n,):
+    if slots is not None and slots.shape != (n,):
         raise OctreeNCAError(f"slots: expected shape {(n,)}, got {tuple(slots.shape)}")
-    st = getattr(lib(), name)(*refs, _ptr(states, model.torch_dtype, "states"), int(from_cell),
-                              math.prod(shape[1:-1]), n, _ptr(slots, torch.int64, "slots"),
-                              int(first), _stream(stream))
+    st = getattr(lib(), name)(*refs, _ptr(states, model.torch_dtype, "states"), from_cell,
+                              states.numel() // (n * c) if n else 0, n,
+                              _ptr(slots, torch.int64, "slots"), first, _stream(stream))
     _check(st, name)
 
 
@@ -626,6 +642,39 @@ def octree_nca_state_cache_read(model: Model, cache: StateCacheBuffers, states, 
     """Fill states [n][...cells][C] with the values of the slots."""
     _cache_call("octree_nca_state_cache_read", model, refs or state_cache_refs(model, cache),
                 states, from_cell, slots, first, stream)
+
+
+def _keep(code, block) -> _Keep:
+    if code not in CODE_NAMES:
+        raise ValueError(f"unknown code {code!r}; known: {sorted(CODE_NAMES)}")
+    return _Keep(CODE_NAMES[code], int(block))
+
+
+def octree_nca_train_kept_workspace_bytes(model: Model, finest, factors, steps, code="i8",
+                                          block=64) -> int:
+    levels = len(steps)
+    return int(lib().octree_nca_train_kept_workspace_bytes(
+        ctypes.byref(model.struct()), _extent(finest), levels, _factors(factors),
+        (_I32 * levels)(*[int(v) for v in steps]), ctypes.byref(_keep(code, block))))
+
+
+def octree_nca_train_step_kept(model: Model, image, factors, weights, steps, fire_rate: float,
+                               seed: int, target, workspace, grads, loss, final_state=None,
+                               code="i8", block=64, stream=None) -> None:
+    """octree_nca_train_step with the states kept in 8 bits (``code``, ``block``)."""
+    levels = len(steps)
+    d, h, w = image.shape[:3]
+    ws = (_LevelWeights * levels)(*[level_weights_struct(x) for x in weights])
+    gs = (_LevelGrads * levels)(*[level_grads_struct(x) for x in grads])
+    s = (_I32 * levels)(*[int(v) for v in steps])
+    st = lib().octree_nca_train_step_kept(
+        ctypes.byref(model.struct()), _ptr(image, torch.float32, "image"), _extent((d, h, w)),
+        levels, _factors(factors), ws, s, float(fire_rate), int(seed),
+        _ptr(target, torch.float32, "target"), ctypes.byref(_keep(code, block)),
+        _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size(), gs,
+        _ptr(loss, torch.float64, "loss"), _ptr(final_state, torch.float32, "final_state"),
+        _stream(stream))
+    _check(st, "octree_nca_train_step_kept")
 
 
 # ---------------------------------------------------------------------------

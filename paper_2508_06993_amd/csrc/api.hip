@@ -1059,6 +1059,44 @@ hipError_t train_forward_step(const StepArgs &a, const void *src, void *dst, hip
     return launch_step_valu(a, src, dst, s);
 }
 
+hipError_t clear_grads(const octnca_model *m, const octnca_level_grads &g, hipStream_t s) {
+    const int64_t c = m->channels, h = m->hidden;
+    float *at[] = {g.conv_w, g.conv_b, g.w1, g.b1, g.w2};
+    const int64_t n[] = {c * (m->ndim == 3 ? 27 : 9), c, h * 2 * c, h, c * h};
+    for (int i = 0; i < 5; ++i) {
+        const hipError_t e = launch_fill_zero(at[i], n[i], s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Forward steps t0 .. t0 + n - 1 of a level: the state after step t goes to
+// dst + (t - t0) states; src is the state before step t0, outside those.
+hipError_t train_forward_run(StepArgs a, int32_t t0, int32_t n, const float *src, float *dst,
+                             hipStream_t s) {
+    const size_t state = (size_t)a.ext.cells() * a.channels;
+    StepBlockPlan blocks;
+    if (step_block_plan(a, true, n, 1, &blocks)) {
+        for (int i = 0, t = 0; i < blocks.launches; ++i) {
+            const int k = blocks.steps_of(i, n);
+            a.step = (uint32_t)(t0 + t);
+            const hipError_t e =
+                launch_step_block(a, true, blocks.tile, k, t == 0 ? src : dst + (t - 1) * state,
+                                  dst + t * state, StepBlockInput{}, s);
+            if (e != hipSuccess) return e;
+            t += k;
+        }
+        return hipSuccess;
+    }
+    for (int32_t t = 0; t < n; ++t) {
+        a.step = (uint32_t)(t0 + t);
+        const hipError_t e =
+            train_forward_step(a, t == 0 ? src : dst + (t - 1) * state, dst + t * state, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1120,23 +1158,8 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
                                   factors[3 * l], factors[3 * l + 1], factors[3 * l + 2], img(l),
                                   tape(l, 0), model->n_in, model->channels, s);
         if (!ok(e)) return OCTNCA_EHIP;
-        StepArgs a = step_args(model, p.ext[l], &weights[l], l, seed, threshold, 0);
-        StepBlockPlan blocks;
-        if (step_block_plan(a, true, steps[l], 1, &blocks)) {
-            for (int i = 0, t = 0; i < blocks.launches; ++i) {
-                const int n = blocks.steps_of(i, steps[l]);
-                a.step = (uint32_t)t;
-                if (!ok(launch_step_block(a, true, blocks.tile, n, tape(l, t), tape(l, t + 1),
-                                          StepBlockInput{}, s)))
-                    return OCTNCA_EHIP;
-                t += n;
-            }
-            continue;
-        }
-        for (int t = 0; t < steps[l]; ++t) {
-            a.step = (uint32_t)t;
-            if (!ok(train_forward_step(a, tape(l, t), tape(l, t + 1), s))) return OCTNCA_EHIP;
-        }
+        const StepArgs a = step_args(model, p.ext[l], &weights[l], l, seed, threshold, 0);
+        if (!ok(train_forward_run(a, 0, steps[l], tape(l, 0), tape(l, 1), s))) return OCTNCA_EHIP;
     }
     const float *final_fine = tape(0, steps[0]);
     float *g = (float *)(ws + p.grad_off[0]);
@@ -1150,16 +1173,8 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
 
     // backward, finest level first; a level's backward writes its weight
     // gradients, so only levels without steps are cleared here
-    const int taps = model->ndim == 3 ? 27 : 9;
-    for (int l = 0; l < levels; ++l) {
-        if (steps[l] > 0) continue;
-        const int64_t c = model->channels, h = model->hidden;
-        const octnca_level_grads &gr = grads[l];
-        if (!ok(launch_fill_zero(gr.conv_w, c * taps, s)) || !ok(launch_fill_zero(gr.conv_b, c, s)) ||
-            !ok(launch_fill_zero(gr.w1, h * 2 * c, s)) || !ok(launch_fill_zero(gr.b1, h, s)) ||
-            !ok(launch_fill_zero(gr.w2, c * h, s)))
-            return OCTNCA_EHIP;
-    }
+    for (int l = 0; l < levels; ++l)
+        if (steps[l] == 0 && !ok(clear_grads(model, grads[l], s))) return OCTNCA_EHIP;
     for (int l = 0; l < levels; ++l) {
         StepArgs a = step_args(model, p.ext[l], &weights[l], l, seed, threshold, 0);
         const LevelGradsDev gd{grads[l].conv_w, grads[l].conv_b, grads[l].w1, grads[l].b1,
@@ -1167,10 +1182,207 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
         // all steps of the level, last first (dL/dS of its first state lands
         // in the other gradient buffer)
         if (steps[l] > 0) {
-            if (!ok(launch_level_backward(a, steps[l], tape(l, 0), g, g_other, gd,
+            if (!ok(launch_level_backward(a, steps[l], false, tape(l, 0), g, g_other, gd,
                                           (float *)(ws + p.bwd_off), s)))
                 return OCTNCA_EHIP;
             std::swap(g, g_other);
+        }
+        if (l + 1 < levels) {
+            if (!ok(launch_upsample_adjoint(g, ext3(p.ext[l + 1]), factors[3 * l],
+                                            factors[3 * l + 1], factors[3 * l + 2], model->n_in,
+                                            model->channels, g_other, s)))
+                return OCTNCA_EHIP;
+            std::swap(g, g_other);
+        }
+    }
+    return OCTNCA_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Workspace of a training step whose states are kept in 8 bits: pyramid images
+// 1..L-1, every level's codes and scales, a window of fp32 states, and the
+// gradient buffers and scratch of TrainPlan.
+struct KeptPlan {
+    octnca_extent ext[kMaxLevels];
+    size_t image_off[kMaxLevels];
+    CacheArgs cache[kMaxLevels];      // offsets in codes / scales until placed
+    size_t code_off[kMaxLevels], scale_off[kMaxLevels];
+    int32_t window[kMaxLevels];       // states of a level that the window holds, even
+    size_t window_off, grad_off[2], bwd_off, mse_off, bytes;
+};
+
+// The window holds kWindowStates of the finest level, and so more of the coarser
+// ones.  A level's forward uses its halves in turn (a run of steps reads the last
+// state of the other half), its backward all of it.
+constexpr int32_t kWindowStates = 4;
+constexpr int32_t kMaxWindow = 32;
+
+int make_kept_plan(const octnca_model *m, octnca_extent finest, int32_t levels,
+                   const int32_t *factors, const int32_t *steps, const octnca_keep *keep,
+                   KeptPlan *p) {
+    TrainPlan t;
+    int st = make_train_plan(m, finest, levels, factors, steps, &t);
+    if (st) return st;
+    if (keep == nullptr || (keep->code != OCTNCA_CODE_I8 && keep->code != OCTNCA_CODE_F8) ||
+        (keep->block != 32 && keep->block != 64 && keep->block != 128))
+        return OCTNCA_EINVAL;
+    const int64_t finest_cells = finest.d * finest.h * finest.w;
+    size_t off = 0;
+    for (int l = 0; l < levels; ++l) {
+        p->ext[l] = t.ext[l];
+        p->image_off[l] = off;
+        const int64_t cells = t.ext[l].d * t.ext[l].h * t.ext[l].w;
+        if (l > 0) off += align_up((size_t)cells * m->n_in * 4);
+        const int64_t room = kWindowStates * (finest_cells / cells);
+        p->window[l] = (int32_t)std::min<int64_t>(room, kMaxWindow) / 2 * 2;
+    }
+    for (int l = 0; l < levels; ++l) {
+        const int64_t cells = t.ext[l].d * t.ext[l].h * t.ext[l].w;
+        CacheArgs a{};
+        a.n_slots = steps[l];
+        a.cells = a.count = cells;
+        a.blocks = (cells + keep->block - 1) / keep->block;
+        a.block = keep->block;
+        a.channels = m->channels;
+        a.f8 = keep->code == OCTNCA_CODE_F8;
+        p->cache[l] = a;
+        p->code_off[l] = off;
+        off += align_up((size_t)steps[l] * cells * m->channels);
+        p->scale_off[l] = off;
+        off += align_up((size_t)steps[l] * a.blocks * m->channels * 4);
+    }
+    p->window_off = off;
+    off += align_up((size_t)kWindowStates * finest_cells * m->channels * 4);
+    // what the other training step has behind its states, unchanged
+    const size_t base = t.grad_off[0];
+    for (int i = 0; i < 2; ++i) p->grad_off[i] = off + (t.grad_off[i] - base);
+    p->bwd_off = off + (t.bwd_off - base);
+    p->mse_off = off + (t.mse_off - base);
+    p->bytes = off + (t.bytes - base);
+    return OCTNCA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t octree_nca_train_kept_workspace_bytes(const octnca_model *model, octnca_extent finest,
+                                             int32_t levels, const int32_t *factors,
+                                             const int32_t *steps, const octnca_keep *keep) {
+    KeptPlan p;
+    return make_kept_plan(model, finest, levels, factors, steps, keep, &p) ? 0 : p.bytes;
+}
+
+int octree_nca_train_step_kept(const octnca_model *model, const void *image, octnca_extent finest,
+                               int32_t levels, const int32_t *factors,
+                               const octnca_level_weights *weights, const int32_t *steps,
+                               float fire_rate, uint64_t seed, const float *target,
+                               const octnca_keep *keep, void *workspace, size_t workspace_bytes,
+                               const octnca_level_grads *grads, double *loss, void *final_state,
+                               void *stream) {
+    KeptPlan p;
+    const int st = make_kept_plan(model, finest, levels, factors, steps, keep, &p);
+    if (st) return st;
+    uint64_t threshold;
+    if (image == nullptr || weights == nullptr || target == nullptr || workspace == nullptr ||
+        grads == nullptr || loss == nullptr || !fire_threshold(fire_rate, &threshold) ||
+        (uintptr_t)workspace % 16)
+        return OCTNCA_EINVAL;
+    for (int l = 0; l < levels; ++l)
+        if (!weights_ok(&weights[l]) || !grads[l].conv_w || !grads[l].conv_b || !grads[l].w1 ||
+            !grads[l].b1 || !grads[l].w2)
+            return OCTNCA_EINVAL;
+    if (workspace_bytes < p.bytes) return OCTNCA_ESPACE;
+    const int64_t cells = finest.d * finest.h * finest.w;
+    const size_t state_bytes = (size_t)cells * model->channels * 4;
+    if (overlap(workspace, p.bytes, image, (size_t)cells * model->n_in * 4) ||
+        overlap(workspace, p.bytes, target, (size_t)cells * 8) ||
+        (final_state && overlap(workspace, p.bytes, final_state, state_bytes)))
+        return OCTNCA_EINVAL;
+
+    const hipStream_t s = (hipStream_t)stream;
+    char *ws = (char *)workspace;
+    auto img = [&](int l) { return l == 0 ? image : (const void *)(ws + p.image_off[l]); };
+    auto ok = [](hipError_t e) { return e == hipSuccess; };
+    float *const window = (float *)(ws + p.window_off);
+    float *const buf[2] = {(float *)(ws + p.grad_off[0]), (float *)(ws + p.grad_off[1])};
+    for (int l = 0; l < levels; ++l) {
+        p.cache[l].codes = (int8_t *)(ws + p.code_off[l]);
+        p.cache[l].scales = (float *)(ws + p.scale_off[l]);
+    }
+    // n states of level l from or to slots first, first + 1, ..
+    auto write = [&](int l, const float *states, int32_t first, int32_t n) {
+        CacheArgs a = p.cache[l];
+        a.first = first;
+        a.n = n;
+        return n == 0 || ok(launch_cache_write(Dtype::F32, a, states, s));
+    };
+    auto read = [&](int l, float *states, int32_t first, int32_t n) {
+        CacheArgs a = p.cache[l];
+        a.first = first;
+        a.n = n;
+        return ok(launch_cache_read(Dtype::F32, a, states, s));
+    };
+
+    // forward: the states before each step go to the cache.  A level starts in
+    // one of the gradient buffers, which are free until the loss; the next level
+    // up starts in the other one, as this one's steps may be none.
+    for (int l = 1; l < levels; ++l) {
+        const int32_t *f = factors + 3 * (l - 1);
+        if (!ok(launch_pool(Dtype::F32, img(l - 1), ext3(p.ext[l]), ws + p.image_off[l], f[0],
+                            f[1], f[2], model->n_in, s)))
+            return OCTNCA_EHIP;
+    }
+    const float *cur = nullptr;   // the last level's last state
+    for (int l = levels - 1; l >= 0; --l) {
+        float *const begin = buf[l & 1];
+        const bool coarsest = l == levels - 1;
+        const int32_t *f = factors + 3 * l;
+        if (!ok(launch_upsample(Dtype::F32, cur, ext3(p.ext[l]), coarsest ? 1 : f[0],
+                                coarsest ? 1 : f[1], coarsest ? 1 : f[2], img(l), begin,
+                                model->n_in, model->channels, s)))
+            return OCTNCA_EHIP;
+        cur = begin;
+        if (steps[l] > 0 && !write(l, begin, 0, 1)) return OCTNCA_EHIP;
+        const StepArgs a = step_args(model, p.ext[l], &weights[l], l, seed, threshold, 0);
+        const size_t state = (size_t)a.ext.cells() * model->channels;
+        const int32_t half = p.window[l] / 2;
+        for (int32_t t = 0, side = 0; t < steps[l]; t += half, side ^= 1) {
+            const int32_t n = std::min(half, steps[l] - t);
+            float *const dst = window + side * half * state;
+            if (!ok(train_forward_run(a, t, n, cur, dst, s)) ||
+                !write(l, dst, t + 1, t + n == steps[l] ? n - 1 : n))   // not the last state
+                return OCTNCA_EHIP;
+            cur = dst + (n - 1) * state;
+        }
+    }
+    float *g = cur == buf[0] ? buf[1] : buf[0];
+    float *g_other = g == buf[0] ? buf[1] : buf[0];
+    if (!ok(launch_readout_mse(cur, target, cells, model->channels, g, loss,
+                               (double *)(ws + p.mse_off), s)))
+        return OCTNCA_EHIP;
+    if (final_state &&
+        !ok(hipMemcpyAsync(final_state, cur, state_bytes, hipMemcpyDeviceToDevice, s)))
+        return OCTNCA_EHIP;
+
+    // backward, finest level first, each level's steps in windows from the last
+    for (int l = 0; l < levels; ++l) {
+        StepArgs a = step_args(model, p.ext[l], &weights[l], l, seed, threshold, 0);
+        const LevelGradsDev gd{grads[l].conv_w, grads[l].conv_b, grads[l].w1, grads[l].b1,
+                               grads[l].w2};
+        if (steps[l] == 0 && !ok(clear_grads(model, grads[l], s))) return OCTNCA_EHIP;
+        for (int32_t end = steps[l]; end > 0;) {
+            const int32_t n = std::min(p.window[l], end);
+            a.step = (uint32_t)(end - n);
+            if (!read(l, window, end - n, n) ||
+                !ok(launch_level_backward(a, n, end < steps[l], window, g, g_other, gd,
+                                          (float *)(ws + p.bwd_off), s)))
+                return OCTNCA_EHIP;
+            std::swap(g, g_other);
+            end -= n;
         }
         if (l + 1 < levels) {
             if (!ok(launch_upsample_adjoint(g, ext3(p.ext[l + 1]), factors[3 * l],

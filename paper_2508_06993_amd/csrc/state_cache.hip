@@ -141,7 +141,7 @@ struct CodeF8 {
 };
 
 constexpr int kWaves = 4;              // per workgroup, each with blocks of its own
-constexpr int64_t kMaxGrid = 1 << 20;  // workgroups along x; the kernels loop over the rest
+constexpr int64_t kMaxGrid = 1 << 23;  // workgroups along x; the kernels loop over the rest
 
 // Work split of the writes: a wave takes whole blocks of cells of one state,
 // whose channel quads lie one after the other in memory.  Lane l takes quads l,
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a,
 
 // A thread takes channel quads of a state, the workgroup's threads apart: 32
 // bytes of the state's values.
-template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
+template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 8;
 template <typename T, int C, typename Code>
 __global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift,
                                                           T *__restrict__ states) {

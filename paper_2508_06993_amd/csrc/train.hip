@@ -884,7 +884,7 @@ hipError_t launch_bwd(const StepArgs &a, const float *src, const float *gout, fl
 // fused, the weight-gradient sums accumulate in the blocks' partial rows, and
 // one bwd_conv_t and one wgrad_reduce finish the level.
 template <int NDIM, int NIN, int C, int H>
-hipError_t launch_bwd_level(const StepArgs &a0, int32_t steps, const float *states,
+hipError_t launch_bwd_level(const StepArgs &a0, int32_t steps, bool add, const float *states,
                             const float *gout, float *gin, LevelGradsDev g, float *ws,
                             hipStream_t stream) {
     const int64_t cells = a0.ext.cells();
@@ -900,7 +900,7 @@ hipError_t launch_bwd_level(const StepArgs &a0, int32_t steps, const float *stat
         int32_t t = steps - 1;
         for (int i = 0; i < plan.launches; ++i) {
             const int n = plan.steps_of(i, steps);
-            a.step = (uint32_t)t;
+            a.step = a0.step + (uint32_t)t;
             const hipError_t e = launch_bwd_block(
                 a, plan, n, states + (size_t)t * cells * C, i == 0 ? gout : gpart[cur ^ 1],
                 i == 0 ? nullptr : gp[cur ^ 1], gpart[cur], gp[cur], partial, i > 0, stream);
@@ -909,11 +909,11 @@ hipError_t launch_bwd_level(const StepArgs &a0, int32_t steps, const float *stat
             t -= n;
         }
         enqueue_tail<NDIM, C, H>(a, gr, gpart[cur ^ 1], gp[cur ^ 1], gin, partial,
-                                 bwd_block_rows(a, plan), true, g, true, stream);
+                                 bwd_block_rows(a, plan), true, g, !add, stream);
         return hipGetLastError();
     }
     for (int32_t t = steps - 1; t >= 0; --t) {
-        a.step = (uint32_t)t;
+        a.step = a0.step + (uint32_t)t;
         const bool first = t == steps - 1;
         enqueue_bwd_cell<NDIM, NIN, C, H>(a, gr, states + (size_t)t * cells * C,
                                           first ? gout : gpart[cur ^ 1],
@@ -922,18 +922,21 @@ hipError_t launch_bwd_level(const StepArgs &a0, int32_t steps, const float *stat
         cur ^= 1;
     }
     enqueue_tail<NDIM, C, H>(a, gr, gpart[cur ^ 1], gp[cur ^ 1], gin, partial, gr.cblocks, false, g,
-                             true, stream);
+                             !add, stream);
     return hipGetLastError();
 }
 
 template <int NDIM, int C, int H>
 hipError_t bwd_nin(const StepArgs &a, const float *src, const float *gout, float *gin,
-                   LevelGradsDev g, float *ws, hipStream_t stream, int32_t level_steps) {
+                   LevelGradsDev g, float *ws, hipStream_t stream, int32_t level_steps,
+                   bool add) {
     if (level_steps >= 0) {
         if (a.n_in == 1)
-            return launch_bwd_level<NDIM, 1, C, H>(a, level_steps, src, gout, gin, g, ws, stream);
+            return launch_bwd_level<NDIM, 1, C, H>(a, level_steps, add, src, gout, gin, g, ws,
+                                                   stream);
         if (a.n_in == 3)
-            return launch_bwd_level<NDIM, 3, C, H>(a, level_steps, src, gout, gin, g, ws, stream);
+            return launch_bwd_level<NDIM, 3, C, H>(a, level_steps, add, src, gout, gin, g, ws,
+                                                   stream);
         return hipErrorInvalidValue;
     }
     if (a.n_in == 1) return launch_bwd<NDIM, 1, C, H>(a, src, gout, gin, g, ws, stream);
@@ -943,13 +946,13 @@ hipError_t bwd_nin(const StepArgs &a, const float *src, const float *gout, float
 
 template <int NDIM>
 hipError_t bwd_size(const StepArgs &a, const float *src, const float *gout, float *gin,
-                    LevelGradsDev g, float *ws, hipStream_t stream, int32_t level_steps) {
+                    LevelGradsDev g, float *ws, hipStream_t stream, int32_t level_steps, bool add) {
     if (a.channels == 16 && a.hidden == 64)
-        return bwd_nin<NDIM, 16, 64>(a, src, gout, gin, g, ws, stream, level_steps);
+        return bwd_nin<NDIM, 16, 64>(a, src, gout, gin, g, ws, stream, level_steps, add);
     if (a.channels == 12 && a.hidden == 48)
-        return bwd_nin<NDIM, 12, 48>(a, src, gout, gin, g, ws, stream, level_steps);
+        return bwd_nin<NDIM, 12, 48>(a, src, gout, gin, g, ws, stream, level_steps, add);
     if (a.channels == 20 && a.hidden == 100)
-        return bwd_nin<NDIM, 20, 100>(a, src, gout, gin, g, ws, stream, level_steps);
+        return bwd_nin<NDIM, 20, 100>(a, src, gout, gin, g, ws, stream, level_steps, add);
     return hipErrorInvalidValue;
 }
 
@@ -1045,16 +1048,16 @@ size_t level_backward_workspace_floats(int ndim, int channels, int hidden, Exten
 
 hipError_t launch_step_backward(const StepArgs &a, const float *src, const float *gout,
                                 float *gin, LevelGradsDev g, float *ws, hipStream_t stream) {
-    return a.ndim == 2 ? bwd_size<2>(a, src, gout, gin, g, ws, stream, -1)
-                       : bwd_size<3>(a, src, gout, gin, g, ws, stream, -1);
+    return a.ndim == 2 ? bwd_size<2>(a, src, gout, gin, g, ws, stream, -1, true)
+                       : bwd_size<3>(a, src, gout, gin, g, ws, stream, -1, true);
 }
 
-hipError_t launch_level_backward(const StepArgs &a, int32_t steps, const float *states,
+hipError_t launch_level_backward(const StepArgs &a, int32_t steps, bool add, const float *states,
                                  const float *gout, float *gin, LevelGradsDev g, float *ws,
                                  hipStream_t stream) {
     if (steps <= 0) return hipSuccess;
-    return a.ndim == 2 ? bwd_size<2>(a, states, gout, gin, g, ws, stream, steps)
-                       : bwd_size<3>(a, states, gout, gin, g, ws, stream, steps);
+    return a.ndim == 2 ? bwd_size<2>(a, states, gout, gin, g, ws, stream, steps, add)
+                       : bwd_size<3>(a, states, gout, gin, g, ws, stream, steps, add);
 }
 
 hipError_t launch_upsample_adjoint(const float *gfine, Extent3 coarse, int fz, int fy, int fx,

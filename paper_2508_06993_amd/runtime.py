@@ -1,6 +1,6 @@
 """Convenience layer over the binding: upload weights, allocate the workspace
-and outputs with PyTorch, run ``octree_nca_infer``.  Allocation and marshalling
-only; the computation is the library's.
+and outputs with PyTorch, run ``octree_nca_infer``; state caches, parameter lists
+and training.  Allocation and marshalling only; the computation is the library's.
 """
 from __future__ import annotations
 
@@ -10,10 +10,12 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (Model, StateCacheBuffers, octree_nca_adamw, octree_nca_clip_grads,
+from . import (Model, OctreeNCAError, StateCacheBuffers, octree_nca_adamw, octree_nca_clip_grads,
                octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
                octree_nca_param_table_bytes, octree_nca_state_cache_read,
-               octree_nca_state_cache_write, octree_nca_workspace_bytes, param_structs,
+               octree_nca_state_cache_write, octree_nca_train_kept_workspace_bytes,
+               octree_nca_train_step, octree_nca_train_step_kept,
+               octree_nca_train_workspace_bytes, octree_nca_workspace_bytes, param_structs,
                state_cache_refs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
@@ -146,3 +148,62 @@ class Parameters:
         octree_nca_adamw(self.list, self.step, lr, betas, eps, weight_decay, max_norm, scale,
                          ema_decay, self.norm, stream)
         return self.norm
+
+
+class Trainer:
+    """Training of one model on images of one extent: gradients of a training
+    step, then the clipped AdamW update of all weights with a running average.
+
+    ``weights``: per level a dict of device fp32 tensors (upload_weights),
+    updated in place; ``ema`` their running averages.  ``keep``: None keeps every
+    state in fp32 (octree_nca_train_step), "i8" or "f8" in 8 bits
+    (octree_nca_train_step_kept), in about half the memory at 20 steps a level
+    and less with more steps."""
+
+    def __init__(self, model: Model, finest: Sequence[int], factors, steps, weights,
+                 keep: Optional[str] = None, block=64, lr=1.6e-3, betas=(0.9, 0.99), eps=1e-8,
+                 weight_decay=0.0, max_norm=float("inf"), ema_decay=0.99):
+        self.model, self.weights, self.keep, self.block = model, weights, keep, block
+        self.finest = tuple(int(v) for v in finest)
+        self.factors = [tuple(int(v) for v in f) for f in factors]
+        self.steps = [int(v) for v in steps]
+        device = weights[0]["w1"].device
+        if keep is None:
+            size = octree_nca_train_workspace_bytes(model, self.finest, self.factors, self.steps)
+        else:
+            size = octree_nca_train_kept_workspace_bytes(model, self.finest, self.factors,
+                                                         self.steps, keep, block)
+        if size == 0:
+            raise OctreeNCAError("Trainer: invalid model, extent, factors or steps")
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
+        like = lambda f: [{k: f(w[k]) for k in WEIGHT_FIELDS} for w in weights]
+        self.grads, self.ema = like(torch.zeros_like), like(torch.clone)
+        m, v = like(torch.zeros_like), like(torch.zeros_like)
+        flat = lambda sets: [s[k] for s in sets for k in WEIGHT_FIELDS]
+        self.parameters = Parameters(flat(self.grads), flat(weights), flat(m), flat(v),
+                                     ema=flat(self.ema))
+        self.settings = dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
+                             max_norm=max_norm, ema_decay=ema_decay)
+        self.loss = torch.zeros(1, dtype=torch.float64, device=device)
+
+    def gradients(self, image: torch.Tensor, target: torch.Tensor, fire_rate: float, seed: int,
+                  final_state=None, stream=None) -> torch.Tensor:
+        """Fills ``grads``; returns the loss (device fp64 [1], overwritten by the next call)."""
+        if self.keep is None:
+            octree_nca_train_step(self.model, image, self.factors, self.weights, self.steps,
+                                  fire_rate, seed, target, self.workspace, self.grads, self.loss,
+                                  final_state, stream)
+        else:
+            octree_nca_train_step_kept(self.model, image, self.factors, self.weights, self.steps,
+                                       fire_rate, seed, target, self.workspace, self.grads,
+                                       self.loss, final_state, self.keep, self.block, stream)
+        return self.loss
+
+    def step(self, image: torch.Tensor, target: torch.Tensor, fire_rate: float, seed: int,
+             stream=None, **settings):
+        """One training step with an update; ``settings`` override the
+        constructor's for this step (lr, ...).  Returns the loss and the
+        gradients' norm before clipping, both on the device."""
+        loss = self.gradients(image, target, fire_rate, seed, stream=stream)
+        norm = self.parameters.adamw(stream=stream, **{**self.settings, **settings})
+        return loss, norm

@@ -13,10 +13,11 @@ import torch
 import paper_2508_06993_amd as octnca
 from paper_2508_06993_amd.runtime import StateCache
 
+from quantise import TINY, e4m3_round, e4m3_values
+
 pytestmark = pytest.mark.gpu
 
 HIDDEN = {12: 48, 16: 64, 20: 100}
-TINY = 2.0 ** -100
 NP = {"f32": np.float32, "f16": np.float16}
 
 
@@ -30,24 +31,6 @@ def states(seed, n, extent, c, dtype):
     x = rng.normal(0, 1, (n,) + extent + (c,)) * np.exp2(np.linspace(-4, 7, c))
     x[..., :3] = rng.uniform(0, 1, (n,) + extent + (3,))
     return x.astype(NP[dtype])
-
-
-def e4m3_values():
-    """Value of each of the 256 codes, from the format's definition."""
-    code = np.arange(256)
-    e, f = (code >> 3) & 15, code & 7
-    v = np.where(e > 0, (1 + f / 8.0) * np.exp2(e - 7.0), f / 8.0 * 2.0 ** -6)
-    v[(code & 127) == 127] = np.nan
-    return np.where(code >> 7, -v, v)
-
-
-def e4m3_round(y):
-    """Nearest e4m3 value, ties to the even code, of |y| <= 448."""
-    v = e4m3_values()[:127]
-    k = np.clip(np.searchsorted(v, np.abs(y)), 1, 126)
-    lo, hi = np.abs(y) - v[k - 1], v[k] - np.abs(y)
-    pick = np.where((lo < hi) | ((lo == hi) & ((k - 1) % 2 == 0)), k - 1, k)
-    return np.copysign(v[pick], y)
 
 
 def blocks_of(x, block):
