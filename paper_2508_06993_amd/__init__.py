@@ -15,6 +15,7 @@ import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
+import numpy as np
 import torch
 
 from .build import LIB_PATH
@@ -690,28 +691,36 @@ def _grad_type(t, name):
     return _GRAD_TYPES[t.dtype]
 
 
+def _addresses(tensors, counts, device, dtype, name):
+    """Addresses of a list of contiguous device tensors of the given sizes."""
+    if len(tensors) != len(counts):
+        raise OctreeNCAError(f"{name}: {len(tensors)} tensors for {len(counts)} gradients")
+    out = [_ptr(t, dtype, name) for t in tensors]
+    for t, n in zip(tensors, counts):
+        if t.numel() != n:
+            raise OctreeNCAError(f"{name}: {t.numel()} elements for {n} of the gradient")
+        if t.device != device:
+            raise OctreeNCAError(f"{name}: on {t.device}, the first gradient on {device}")
+    return out
+
+
 def param_structs(grads, params=None, m=None, v=None, ema=None, clipped=None):
     """Array of octnca_param for lists of device tensors (index = tensor)."""
-    n = len(grads)
-    lists = {"clipped": clipped, "param": params, "m": m, "v": v, "ema": ema}
-    for k, x in lists.items():
-        if x is not None and len(x) != n:
-            raise OctreeNCAError(f"{k}: {len(x)} tensors for {n} gradients")
-    out = (_Param * max(1, n))()
-    for i, g in enumerate(grads):
-        p = out[i]
-        p.count, p.grad, p.grad_dtype = g.numel(), _ptr(g, None, "grad"), _grad_type(g, "grad")
-        for k, x in lists.items():
-            if x is None:
-                continue
-            if x[i].numel() != p.count:
-                raise OctreeNCAError(f"{k}: {x[i].numel()} elements for {p.count} of the gradient")
-            if x[i].device != g.device:
-                raise OctreeNCAError(f"{k}: on {x[i].device}, the gradient on {g.device}")
-            setattr(p, k, _ptr(x[i], None if k == "clipped" else torch.float32, k))
-        if clipped is not None:
-            p.clipped_dtype = _grad_type(clipped[i], "clipped")
-    return out
+    if not grads:
+        return (_Param * 1)()
+    counts = [g.numel() for g in grads]
+    device = grads[0].device
+    out = np.zeros(len(grads), np.dtype(_Param))
+    out["count"] = counts
+    out["grad"] = _addresses(grads, counts, device, None, "grad")
+    out["grad_dtype"] = [_grad_type(g, "grad") for g in grads]
+    for k, x in (("param", params), ("m", m), ("v", v), ("ema", ema)):
+        if x is not None:
+            out[k] = _addresses(x, counts, device, torch.float32, k)
+    if clipped is not None:
+        out["clipped"] = _addresses(clipped, counts, device, None, "clipped")
+        out["clipped_dtype"] = [_grad_type(t, "clipped") for t in clipped]
+    return (_Param * len(grads)).from_buffer(out)
 
 
 def octree_nca_param_table_bytes(structs, n: int) -> int:

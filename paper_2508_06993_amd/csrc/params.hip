@@ -43,10 +43,10 @@ Chunk *chunks_of(void *table) { return (Chunk *)((char *)table + sizeof(Scratch)
 
 // --- the table ---------------------------------------------------------------
 
-constexpr int kFillTensors = 48;   // a launch's tensors travel in its arguments
+constexpr int kFillTensors = 52;   // a launch's tensors travel in its arguments
 struct FillArgs {
     octnca_param t[kFillTensors];
-    int n;
+    uint32_t at[kFillTensors];   // first record of each, from the launch's first
 };
 static_assert(sizeof(FillArgs) <= 4096 - 64, "kernel arguments");
 
@@ -68,34 +68,31 @@ __host__ __device__ inline int64_t pieces_of(const octnca_param &t) {
     return (t.count + (lead > 0 ? lead : 0) + kParamChunk - 1) / kParamChunk;
 }
 
-// Records of the tensors of `f`, from record `at` on.
+// Records of the tensors of `f`, one per blockIdx.y, from record `at` on.
 __global__ __launch_bounds__(kThreads) void fill_table(FillArgs f, Scratch *scratch, Chunk *chunks,
                                                        int64_t at) {
-    const int64_t thread = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t threads = (int64_t)gridDim.x * kThreads;
-    if (thread == 0) scratch->done = 0;
-    for (int i = 0; i < f.n; ++i) {
-        const octnca_param &t = f.t[i];
-        const int lead = lead_of(t);
-        const int64_t skip = lead > 0 ? lead : 0;
-        const int64_t total = t.count + skip, pieces = pieces_of(t);
-        for (int64_t k = thread; k < pieces; k += threads) {
-            const int64_t e = k * kParamChunk - skip;   // the aligned start
-            Chunk c;
-            c.grad = (const char *)t.grad + e * bytes_of(t.grad_dtype);
-            c.clipped = t.clipped ? (char *)t.clipped + e * bytes_of(t.clipped_dtype) : nullptr;
-            c.param = t.param ? t.param + e : nullptr;
-            c.m = t.m ? t.m + e : nullptr;
-            c.v = t.v ? t.v + e : nullptr;
-            c.ema = t.ema ? t.ema + e : nullptr;
-            c.first = k == 0 ? (int32_t)skip : 0;
-            const int64_t left = total - k * kParamChunk;
-            c.end = (int32_t)(left < kParamChunk ? left : kParamChunk);
-            c.types = t.grad_dtype | (t.clipped ? t.clipped_dtype << 8 : 0);
-            c.quads = lead >= 0;
-            chunks[at + k] = c;
-        }
-        at += pieces;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) scratch->done = 0;
+    const octnca_param &t = f.t[blockIdx.y];
+    if (t.count == 0) return;
+    const int lead = lead_of(t);
+    const int64_t skip = lead > 0 ? lead : 0;
+    const int64_t total = t.count + skip, pieces = pieces_of(t);
+    for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < pieces;
+         k += (int64_t)gridDim.x * kThreads) {
+        const int64_t e = k * kParamChunk - skip;   // the aligned start
+        Chunk c;
+        c.grad = (const char *)t.grad + e * bytes_of(t.grad_dtype);
+        c.clipped = t.clipped ? (char *)t.clipped + e * bytes_of(t.clipped_dtype) : nullptr;
+        c.param = t.param ? t.param + e : nullptr;
+        c.m = t.m ? t.m + e : nullptr;
+        c.v = t.v ? t.v + e : nullptr;
+        c.ema = t.ema ? t.ema + e : nullptr;
+        c.first = k == 0 ? (int32_t)skip : 0;
+        const int64_t left = total - k * kParamChunk;
+        c.end = (int32_t)(left < kParamChunk ? left : kParamChunk);
+        c.types = t.grad_dtype | (t.clipped ? t.clipped_dtype << 8 : 0);
+        c.quads = lead >= 0;
+        chunks[at + f.at[blockIdx.y] + k] = c;
     }
 }
 
@@ -516,7 +513,11 @@ __global__ __launch_bounds__(kSmallThreads) void small_adamw(Scratch *scratch, c
                                                              int n, UpdateArgs u, double beta1,
                                                              double beta2, int64_t *step,
                                                              float *norm) {
-    const int64_t t = __hip_atomic_load(step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    // One thread reads *step, before the sum's barrier (the last one: its wave has
+    // the least to sum), and leaves it in LDS.
+    __shared__ int64_t now;
+    if (threadIdx.x == kSmallThreads - 1)
+        now = __hip_atomic_load(step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
     Chunk c{};
     if (n > 0) c = chunks[blockIdx.x];
     with_type(c.grad_dtype(), [&](auto type) {
@@ -527,10 +528,11 @@ __global__ __launch_bounds__(kSmallThreads) void small_adamw(Scratch *scratch, c
         if (whole) own.load(c, q);
         const double len = small_norm(chunks, n, u.scale);
         const bool fine = __builtin_isfinite(len);
+        const int64_t t = now;
         if (threadIdx.x == 0) {
             if (norm && blockIdx.x == 0) *norm = (float)len;
             // The workgroup that counts last writes *step: the others have read
-            // it before they counted (acq_rel).
+            // it before they counted.
             const uint32_t before = __hip_atomic_fetch_add(&scratch->done, 1u, __ATOMIC_ACQ_REL,
                                                            __HIP_MEMORY_SCOPE_AGENT);
             if (before == gridDim.x - 1) {
@@ -584,15 +586,19 @@ hipError_t launch_param_table(const octnca_param *params, int n, void *table, hi
     int64_t at = 0;
     int i = 0;
     do {   // once at least: an empty list has scratch memory too
-        FillArgs f;
-        int64_t pieces = 0;
-        for (f.n = 0; i < n && f.n < kFillTensors; ++i) {
+        FillArgs f{};
+        int64_t pieces = 0, most = 1;
+        int m = 0;
+        for (; i < n && m < kFillTensors; ++i) {
             if (params[i].count == 0) continue;
-            f.t[f.n++] = params[i];
-            pieces += pieces_of(params[i]);
+            const int64_t own = pieces_of(params[i]);
+            f.t[m] = params[i];
+            f.at[m++] = (uint32_t)pieces;
+            pieces += own;
+            most = std::max(most, own);
         }
-        const unsigned grid =
-            (unsigned)std::min<int64_t>((pieces + kThreads) / kThreads, 256);
+        const dim3 grid((unsigned)std::min<int64_t>((most + kThreads - 1) / kThreads, 256),
+                        (unsigned)std::max(m, 1));
         fill_table<<<grid, kThreads, 0, stream>>>(f, scratch_of(table), chunks_of(table), at);
         at += pieces;
     } while (i < n);

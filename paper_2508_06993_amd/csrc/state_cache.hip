@@ -197,13 +197,16 @@ __device__ __forceinline__ void quad_max(Words4 (*peers)[64], Words4 (*tops)[Q],
     wave_fence();
 }
 
-// Slot of state i; whether it is one of the cache's.
+// Slot of state i; whether it is one of the cache's (0 if not).
 __device__ __forceinline__ bool slot_of(const CacheArgs &a, int i, int64_t &slot) {
     slot = a.slots ? a.slots[i] : a.first + i;
-    return slot >= 0 && slot < a.n_slots;
+    const bool there = slot >= 0 && slot < a.n_slots;
+    if (!there) slot = 0;
+    return there;
 }
 
-// Whether a later entry of `slots` names the same slot (then that one is kept).
+// Whether a later entry of `slots` names the same slot (then that one is kept):
+// the wave's lanes look at 64 entries at a time.
 __device__ __forceinline__ bool written_later(const CacheArgs &a, int i, int64_t slot) {
     if (!a.slots) return false;
     bool found = false;
