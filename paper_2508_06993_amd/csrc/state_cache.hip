@@ -312,26 +312,29 @@ __device__ __forceinline__ void write_blocks(const CacheArgs &a, int i, int64_t 
 }
 
 // A wave takes N consecutive blocks at a time, with all their loads in flight.
-// The values stay in registers between the maxima and the codes.
+// The values stay in registers between the maxima and the codes.  A state has
+// `full` groups of N B cells and one of `tail` cells (0: none).  Both come as
+// arguments: with the group's cells as a 64-bit minimum in the kernel, this
+// compiler (ROCm 7.2) selected between them by a carry flag that the comparison
+// had not set, and the tail was taken for a full group.
 template <typename T, int C, int B, int N, typename Code>
-__global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a,
+__global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t full, int tail,
                                                            const T *__restrict__ states) {
     __shared__ Words4 peers[kWaves][N][64];
     __shared__ Words4 tops[kWaves][N][C / 4];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
         const T *from = states + (int64_t)i * a.count * C;
-        for (int64_t g = (int64_t)blockIdx.x * kWaves + wave; g * N * B < a.count;
-             g += (int64_t)gridDim.x * kWaves) {
-            const int64_t cell = g * N * B;
-            const int cells = (int)std::min<int64_t>(a.count - cell, N * B);
-            if (cells == N * B)
+        const uint32_t groups = full + (tail > 0);
+        for (uint32_t g = blockIdx.x * kWaves + wave; g < groups; g += gridDim.x * kWaves) {
+            const int64_t cell = (int64_t)g * (N * B);
+            if (g < full)
                 with_flag(a.stream, [&](auto stream) {
                     write_blocks<T, C, B, N, Code, true, decltype(stream)::value>(
-                        a, i, cell, cells, from + cell * C, peers[wave], tops[wave]);
+                        a, i, cell, N * B, from + cell * C, peers[wave], tops[wave]);
                 });
             else
-                write_blocks<T, C, B, N, Code, false, false>(a, i, cell, cells, from + cell * C,
+                write_blocks<T, C, B, N, Code, false, false>(a, i, cell, tail, from + cell * C,
                                                              peers[wave], tops[wave]);
         }
     }
@@ -339,44 +342,44 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a,
 
 // A thread takes channel quads of a state, the workgroup's threads apart: 32
 // bytes of the state's values.
-template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 8;
+template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int C, typename Code>
-__global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift,
-                                                          T *__restrict__ states) {
+__global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift, uint32_t full,
+                                                          int tail, T *__restrict__ states) {
     constexpr int kQ = C / 4, kThreads = 64 * kWaves, kN = kReadQuads<T>;
     using Raw = typename Quad<T>::Raw;
-    const int64_t quads = a.count * kQ;
     for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
         int64_t slot;
         const bool there = slot_of(a, i, slot);
         Raw *to = (Raw *)(states + (int64_t)i * a.count * C);
         const uint32_t *codes = (const uint32_t *)(a.codes + (slot * a.cells + a.from) * C);
         const float4 *scales = (const float4 *)(a.scales + (slot * a.blocks + (a.from >> shift)) * C);
-        for (int64_t base = (int64_t)blockIdx.x * kN * kThreads; base < quads;
-             base += (int64_t)gridDim.x * kN * kThreads) {
-            const int left = (int)std::min<int64_t>(quads - base, kN * kThreads);
+        const uint32_t tiles = full + (tail > 0);   // of kN kThreads quads; the last of `tail`
+        for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            const int64_t base = (int64_t)tile * (kN * kThreads);
+            const int left = tile < full ? kN * kThreads : tail;
             const int64_t cell = base / kQ;                 // of the first quad, and its place in it
             const int over = (int)(base - cell * kQ);
-            uint32_t code[kN] = {};
-            float4 s[kN] = {};
-            if (there)
-                with_flag(a.stream, [&](auto stream) {
+            // past the tile's end a thread reads its last quad once more: no
+            // branches among the loads
+            uint32_t code[kN];
+            float4 s[kN];
+            with_flag(a.stream, [&](auto stream) {
+                if (there) {
 #pragma unroll
                     for (int k = 0; k < kN; ++k) {
-                        const int q = threadIdx.x + k * kThreads;
-                        if (q >= left) continue;
+                        const int q = std::min((int)threadIdx.x + k * kThreads, left - 1);
                         code[k] = get<decltype(stream)::value>(codes + base + q);
                         const int c = (q + over) / kQ;
                         s[k] = scales[((cell + c) >> shift) * kQ + (q + over - c * kQ)];
                     }
-                });
-            with_flag(a.stream, [&](auto stream) {
+                }
 #pragma unroll
                 for (int k = 0; k < kN; ++k) {
                     const int q = threadIdx.x + k * kThreads;
                     const float scale[4] = {s[k].x, s[k].y, s[k].z, s[k].w};
-                    float x[4];
-                    Code::decode(code[k], scale, x);
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (there) Code::decode(code[k], scale, x);
                     if (q < left) put<decltype(stream)::value>(to + base + q, Quad<T>::pack(x));
                 }
             });
@@ -388,7 +391,8 @@ template <typename T, int C, int B, int N, typename Code>
 hipError_t launch_write(const CacheArgs &a, const void *states, hipStream_t stream) {
     const int64_t groups = (a.count + (int64_t)B * N * kWaves - 1) / (B * N * kWaves);
     const dim3 grid((unsigned)std::min(groups, kMaxGrid), (unsigned)std::min(a.n, 65535));
-    cache_write<T, C, B, N, Code><<<grid, 64 * kWaves, 0, stream>>>(a, (const T *)states);
+    cache_write<T, C, B, N, Code><<<grid, 64 * kWaves, 0, stream>>>(
+        a, (uint32_t)(a.count / (N * B)), (int)(a.count % (N * B)), (const T *)states);
     return hipGetLastError();
 }
 
@@ -415,7 +419,9 @@ hipError_t run(CacheArgs a, bool write, void *states, hipStream_t stream) {
         const int64_t groups = (a.count * (C / 4) + per - 1) / per;
         const dim3 grid((unsigned)std::min(groups, kMaxGrid), (unsigned)std::min(a.n, 65535));
         const int shift = a.block == 32 ? 5 : a.block == 64 ? 6 : 7;
-        cache_read<T, C, Code><<<grid, 64 * kWaves, 0, stream>>>(a, shift, (T *)states);
+        cache_read<T, C, Code><<<grid, 64 * kWaves, 0, stream>>>(
+            a, shift, (uint32_t)(a.count * (C / 4) / per), (int)(a.count * (C / 4) % per),
+            (T *)states);
         return hipGetLastError();
     }
     switch (a.block) {

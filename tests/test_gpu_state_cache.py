@@ -252,6 +252,35 @@ def test_offsets_past_32_bits(gpu):
     assert float((x[1] - want).abs().max()) <= float(part.abs().max()) / 254 * 1.001
 
 
+@pytest.mark.parametrize("c,dtype,kind,block", [(16, "f32", "i8", 64), (12, "f32", "f8", 32),
+                                                (20, "f16", "i8", 32), (16, "f16", "f8", 128),
+                                                (12, "f16", "i8", 64), (16, "f16", "f8", 32)])
+def test_large_calls_equal_small_ones(gpu, c, dtype, kind, block):
+    """A call of more states than the last-level cache holds gives the bits of
+    one call per state, written and read; ragged blocks and rows that are not
+    finite included."""
+    m = model(c, dtype)
+    extent, n = (1, 613, 1021), 6
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    x = (torch.randn((n,) + extent + (c,), generator=gen, device="cuda") * 3).to(m.torch_dtype)
+    x[2, 0, 7] = float("nan")
+    x[4, 0, 600:, :, 1] = float("inf")
+    big, one = (StateCache(m, extent, n, kind, block) for _ in range(2))
+    slots = torch.tensor([3, 0, 5, 1, 4, 2], dtype=torch.int64, device="cuda")
+    big.write(x, slots)
+    for i in range(n):
+        one.write(x[i:i + 1], first=int(slots[i]))
+    torch.cuda.synchronize()
+    assert torch.equal(big.buffers.codes, one.buffers.codes)
+    assert torch.equal(big.buffers.scales, one.buffers.scales)
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    big.read(a, slots)
+    for i in range(n):
+        one.read(b[i:i + 1], first=int(slots[i]))
+    raw = torch.int32 if dtype == "f32" else torch.int16
+    assert torch.equal(a.view(raw), b.view(raw))
+
+
 def test_another_stream_and_a_graph(gpu):
     """Calls on a stream of their own, and captured into a graph that is
     replayed with new contents."""
