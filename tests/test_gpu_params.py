@@ -206,6 +206,40 @@ def test_adamw_leaves_out_a_step_that_overflowed(gpu, bad, dtype):
     assert not np.array_equal(before[0], f64(p))
 
 
+@pytest.mark.parametrize("dtype,gap", [("f32", 1), ("bf16", 64)])
+def test_large_lists(gpu, dtype, gap):
+    """Lists larger than the last-level cache, of tensors from one element to
+    millions, against 64 bits on the GPU; several chunks a workgroup."""
+    counts = [1 + (977 * k) % 60013 for k in range(300)] + [9_000_001, 16_777_216, 5, 4_000_003]
+    g = make(counts, dtype, 40, gap, 0.01, head=1 % gap)
+    p, m, v, ema, o = (make(counts, "f32", 41 + k, gap, 0.1, head=1 % gap) for k in range(5))
+    cat = lambda x: torch.cat([t.double() for t in x])
+    for t in v:
+        t.square_()
+    want = cat(g)
+    n = float(torch.dot(want, want)) ** 0.5
+    lst = Parameters(g, p, m, v, ema=ema, clipped=o)
+    assert abs(float(lst.grad_norm(0.5)) - 0.5 * n) <= 2.0 ** -23 * n
+    assert abs(float(lst.clip(0.75, 0.5)) - 0.5 * n) <= 2.0 ** -23 * n
+    f = 0.75 / n
+    assert bool(((cat(o) - want * f).abs() <= 2.0 ** -22 * (want * f).abs() + 2.0 ** -149).all())
+    before = [cat(x) for x in (p, m, v, ema)]
+    lst.adamw(1e-2, (0.9, 0.99), 1e-8, 0.01, max_norm=0.75, ema_decay=0.9)
+    x, lr, u = want * f, 1e-2, 2.0 ** -24
+    m1, v1 = 0.9 * before[1] + 0.1 * x, 0.99 * before[2] + 0.01 * x * x
+    assert bool(((cat(m) - m1).abs() <= 16 * u * (before[1].abs() + x.abs())).all())
+    assert bool(((cat(v) - v1).abs() <= 16 * u * v1).all())
+    root = (v1 / (1 - 0.99)).sqrt() + 1e-8
+    d = (m1 / (1 - 0.9)) / root
+    p1 = before[0] - lr * (d + 0.01 * before[0])
+    # the first moment's terms may cancel; the rest is relative to d and p
+    ep = 16 * u * (lr * (d.abs() + 10 * (before[1].abs() + x.abs()) / root) + p1.abs() + lr)
+    assert bool(((cat(p) - p1).abs() <= ep).all())
+    e1 = 0.9 * before[3] + 0.1 * p1
+    assert bool(((cat(ema) - e1).abs() <= ep + 16 * u * (before[3].abs() + p1.abs())).all())
+    assert int(lst.step) == 1 and bool((cat(g) == want).all())
+
+
 def test_results_do_not_depend_on_the_run(gpu):
     """The same bits again: no order of additions is left to chance."""
     outs = []
