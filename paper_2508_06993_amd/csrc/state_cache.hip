@@ -1,5 +1,17 @@
 // State cache: states in 8 bits with a scale for each block of cells and
 // channel (formulas in octree_nca.h).
+//
+// Both directions are one pass over memory: a write reads a value once and
+// leaves one byte of it, a read the reverse, and a block's scales add 4 bytes per
+// channel.  A 184.5M-cell fp32 state (11.8 GB, blocks of 64) is written in 2.56
+// ms and read back in 2.50 ms, 5.9 TB/s of these bytes each (counters show no
+// others); a copy of 8 GB reaches 4.4 TB/s on this card and reading alone 6.3.
+// What took the writes there from 3.0 TB/s: the values stay in registers between
+// the block's maxima and its codes (one read instead of two), the maxima are
+// unsigned maxima of the magnitudes' bits (a comparison for finite values only
+// where a block has others), one lane per channel divides, and calls larger than
+// the last-level cache go past it.  Small calls are bound by their launches: a
+// 320 x 320 state 4.1 us each way.
 #include <algorithm>
 #include <type_traits>
 
@@ -341,7 +353,9 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t
 }
 
 // A thread takes channel quads of a state, the workgroup's threads apart: 32
-// bytes of the state's values.
+// bytes of the state's values (of one quad a thread fp16 states were read at 3.0
+// TB/s, of four at 5.5).  The workgroups do not loop: a grid of 2048 that loop
+// over a 184.5M-cell state took 3.1 ms instead of 2.5.
 template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int C, typename Code>
 __global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift, uint32_t full,
