@@ -3,14 +3,14 @@
 //
 // Both directions are one pass over memory: a write reads a value once and
 // leaves one byte of it, a read the reverse, and a block's scales add 4 bytes per
-// channel.  A 184.5M-cell fp32 state (11.8 GB, blocks of 64) is written in 2.56
-// ms and read back in 2.50 ms, 5.9 TB/s of these bytes each (counters show no
+// channel.  A 184.5M-cell fp32 state (11.8 GB, blocks of 64) is written in 2.43
+// ms and read back in 2.49 ms, 6.1 TB/s of these bytes each (counters show no
 // others); a copy of 8 GB reaches 4.4 TB/s on this card and reading alone 6.3.
 // What took the writes there from 3.0 TB/s: the values stay in registers between
 // the block's maxima and its codes (one read instead of two), the maxima are
 // unsigned maxima of the magnitudes' bits (a comparison for finite values only
-// where a block has others), one lane per channel divides, and calls larger than
-// the last-level cache go past it.  Small calls are bound by their launches: a
+// where a block has others), one lane per channel divides, the slot list is on its
+// way with the values, and calls larger than the last-level cache go past it.  Small calls are bound by their launches: a
 // 320 x 320 state 4.1 us each way.
 #include <algorithm>
 #include <type_traits>
@@ -209,22 +209,31 @@ __device__ __forceinline__ void quad_max(Words4 (*peers)[64], Words4 (*tops)[Q],
     wave_fence();
 }
 
-// Slot of state i; whether it is one of the cache's (0 if not).
-__device__ __forceinline__ bool slot_of(const CacheArgs &a, int i, int64_t &slot) {
-    slot = a.slots ? a.slots[i] : a.first + i;
-    const bool there = slot >= 0 && slot < a.n_slots;
-    if (!there) slot = 0;
-    return there;
-}
+// What the caller's list says of state i: its slot, and (writes) the entries
+// after it, 64 of them a lane each.  Loaded ahead of the values, used after.
+struct SlotEntry {
+    int64_t slot, later;
 
-// Whether a later entry of `slots` names the same slot (then that one is kept):
-// the wave's lanes look at 64 entries at a time.
-__device__ __forceinline__ bool written_later(const CacheArgs &a, int i, int64_t slot) {
-    if (!a.slots) return false;
-    bool found = false;
-    for (int j = i + 1 + (threadIdx.x & 63); j < a.n; j += 64) found |= a.slots[j] == slot;
-    return __any(found);
-}
+    __device__ __forceinline__ SlotEntry(const int64_t *__restrict__ slots, const CacheArgs &a,
+                                         int i, bool write) {
+        const int j = i + 1 + (threadIdx.x & 63);
+        slot = slots ? slots[i] : a.first + i;
+        later = write && slots && j < a.n ? slots[j] : -1;
+    }
+
+    __device__ __forceinline__ bool in_cache(const CacheArgs &a) const {
+        return slot >= 0 && slot < a.n_slots;
+    }
+
+    // Whether a later entry names the same slot (then that one is kept).
+    __device__ __forceinline__ bool written_later(const int64_t *__restrict__ slots,
+                                                  const CacheArgs &a, int i) const {
+        if (!slots) return false;
+        bool found = later == slot;
+        for (int j = i + 65 + (threadIdx.x & 63); j < a.n; j += 64) found |= slots[j] == slot;
+        return __any(found);
+    }
+};
 
 // Calls f with `flag` as a constant.
 template <typename F> __device__ __forceinline__ void with_flag(bool flag, F f) {
@@ -238,7 +247,8 @@ template <typename F> __device__ __forceinline__ void with_flag(bool flag, F f) 
 // them, src: their first) by one wave; FULL: cells = N B.  LDS of the wave:
 // peers, tops.
 template <typename T, int C, int B, int N, typename Code, bool FULL, bool STREAM>
-__device__ __forceinline__ void write_blocks(const CacheArgs &a, int i, int64_t cell, int cells,
+__device__ __forceinline__ void write_blocks(const CacheArgs &a, const int64_t *__restrict__ slots,
+                                             const SlotEntry &entry, int i, int64_t cell, int cells,
                                              const T *src_cells, Words4 (*peers)[64],
                                              Words4 (*tops)[C / 4]) {
     using S = Split<C, B>;
@@ -272,9 +282,8 @@ __device__ __forceinline__ void write_blocks(const CacheArgs &a, int i, int64_t 
         m[b] = top.bits();
     }
     quad_max<S::kQ, S::kPeers, N>(peers, tops, m);
-    // the slot is looked up behind the loads, which do not need it
-    int64_t slot;
-    if (!slot_of(a, i, slot) || written_later(a, i, slot)) return;
+    if (!entry.in_cache(a) || entry.written_later(slots, a, i)) return;
+    const int64_t slot = entry.slot;
     float *scales = a.scales + (slot * a.blocks + (a.from + cell) / B) * C;
     // one lane a channel and block: its factor takes its maximum's place
     uint32_t *values = (uint32_t *)tops;
@@ -331,6 +340,7 @@ __device__ __forceinline__ void write_blocks(const CacheArgs &a, int i, int64_t 
 // had not set, and the tail was taken for a full group.
 template <typename T, int C, int B, int N, typename Code>
 __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t full, int tail,
+                                                           const int64_t *__restrict__ slots,
                                                            const T *__restrict__ states) {
     __shared__ Words4 peers[kWaves][N][64];
     __shared__ Words4 tops[kWaves][N][C / 4];
@@ -340,14 +350,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t
         const uint32_t groups = full + (tail > 0);
         for (uint32_t g = blockIdx.x * kWaves + wave; g < groups; g += gridDim.x * kWaves) {
             const int64_t cell = (int64_t)g * (N * B);
+            const SlotEntry entry(slots, a, i, true);
             if (g < full)
                 with_flag(a.stream, [&](auto stream) {
                     write_blocks<T, C, B, N, Code, true, decltype(stream)::value>(
-                        a, i, cell, N * B, from + cell * C, peers[wave], tops[wave]);
+                        a, slots, entry, i, cell, N * B, from + cell * C, peers[wave],
+                        tops[wave]);
                 });
             else
-                write_blocks<T, C, B, N, Code, false, false>(a, i, cell, tail, from + cell * C,
-                                                             peers[wave], tops[wave]);
+                write_blocks<T, C, B, N, Code, false, false>(
+                    a, slots, entry, i, cell, tail, from + cell * C, peers[wave], tops[wave]);
         }
     }
 }
@@ -359,12 +371,15 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t
 template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int C, typename Code>
 __global__ __launch_bounds__(64 * kWaves) void cache_read(CacheArgs a, int shift, uint32_t full,
-                                                          int tail, T *__restrict__ states) {
+                                                          int tail,
+                                                          const int64_t *__restrict__ slots,
+                                                          T *__restrict__ states) {
     constexpr int kQ = C / 4, kThreads = 64 * kWaves, kN = kReadQuads<T>;
     using Raw = typename Quad<T>::Raw;
     for (int i = blockIdx.y; i < a.n; i += gridDim.y) {
-        int64_t slot;
-        const bool there = slot_of(a, i, slot);
+        const SlotEntry entry(slots, a, i, false);
+        const bool there = entry.in_cache(a);
+        const int64_t slot = there ? entry.slot : 0;
         Raw *to = (Raw *)(states + (int64_t)i * a.count * C);
         const uint32_t *codes = (const uint32_t *)(a.codes + (slot * a.cells + a.from) * C);
         const float4 *scales = (const float4 *)(a.scales + (slot * a.blocks + (a.from >> shift)) * C);
@@ -406,7 +421,8 @@ hipError_t launch_write(const CacheArgs &a, const void *states, hipStream_t stre
     const int64_t groups = (a.count + (int64_t)B * N * kWaves - 1) / (B * N * kWaves);
     const dim3 grid((unsigned)std::min(groups, kMaxGrid), (unsigned)std::min(a.n, 65535));
     cache_write<T, C, B, N, Code><<<grid, 64 * kWaves, 0, stream>>>(
-        a, (uint32_t)(a.count / (N * B)), (int)(a.count % (N * B)), (const T *)states);
+        a, (uint32_t)(a.count / (N * B)), (int)(a.count % (N * B)), a.slots,
+        (const T *)states);
     return hipGetLastError();
 }
 
@@ -435,7 +451,7 @@ hipError_t run(CacheArgs a, bool write, void *states, hipStream_t stream) {
         const int shift = a.block == 32 ? 5 : a.block == 64 ? 6 : 7;
         cache_read<T, C, Code><<<grid, 64 * kWaves, 0, stream>>>(
             a, shift, (uint32_t)(a.count * (C / 4) / per), (int)(a.count * (C / 4) % per),
-            (T *)states);
+            a.slots, (T *)states);
         return hipGetLastError();
     }
     switch (a.block) {

@@ -269,12 +269,13 @@ def test_guard_values_stay(gpu):
             assert not bool((b[start:start + n] == 5).any())
 
 
-def test_another_stream_and_a_graph(gpu):
+@pytest.mark.parametrize("name", ["model", "sizes"])
+def test_another_stream_and_a_graph(gpu, name):
     """A list used on a stream of its own, and captured: the replays go on
-    counting steps and see new gradients."""
+    counting steps and see new gradients; lists of one launch and of two."""
     def lists():
-        g = make(COUNTS, "f32", 30)
-        p, m, v = (make(COUNTS, "f32", 31 + k) for k in range(3))
+        g = make(LISTS[name], "f32", 30)
+        p, m, v = (make(LISTS[name], "f32", 31 + k) for k in range(3))
         return g, p, Parameters(g, p, m, [x.square_() for x in v])
     g1, p1, eager = lists()
     g2, p2, other = lists()
