@@ -23,6 +23,7 @@ namespace {
 constexpr int64_t kMaxDim = int64_t(1) << 30;      // per axis (kernels index with int)
 constexpr int64_t kMaxCells = int64_t(1) << 36;    // per level
 constexpr int kMaxLevels = 16;
+constexpr int64_t kMaxCacheBytes = int64_t(1) << 60;
 constexpr int kMaxGroup = 64;   // images of a batch that run together at most
 constexpr size_t kAlign = 256;
 
@@ -1241,6 +1242,8 @@ int make_kept_plan(const octnca_model *m, octnca_extent finest, int32_t levels,
     }
     for (int l = 0; l < levels; ++l) {
         const int64_t cells = t.ext[l].d * t.ext[l].h * t.ext[l].w;
+        // no sum of the sizes below leaves 64 bits
+        if (steps[l] > kMaxCacheBytes / kMaxLevels / (cells * m->channels * 5)) return OCTNCA_ESHAPE;
         CacheArgs a{};
         a.n_slots = steps[l];
         a.cells = a.count = cells;
@@ -1398,8 +1401,6 @@ int octree_nca_train_step_kept(const octnca_model *model, const void *image, oct
 }  // extern "C"
 
 namespace {
-
-constexpr int64_t kMaxCacheBytes = int64_t(1) << 60;
 
 // Checks a cache and a call's range; fills the kernels' arguments.
 int make_cache_args(const octnca_model *m, const octnca_state_cache *c, const void *states,

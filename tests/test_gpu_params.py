@@ -174,6 +174,35 @@ def test_adamw(gpu, dtype, with_ema, decay, name, gap):
         assert np.array_equal(f64(g), before[0])
 
 
+@pytest.mark.parametrize("counts", [[143, 17, 2047, 65, 1023] * 4, [50_001, 7, 12_288, 1, 30_000]],
+                         ids=["one-launch", "two-launches"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads", [(0, 0, 0, 0, 0, 0), (3, 3, 3, 3, 3, 3), (1, 2, 3, 0, 1, 2),
+                                   (0, 0, 0, 0, 0, 1)])
+def test_arrays_at_any_element(gpu, counts, dtype, heads):
+    """The arrays of a tensor at the same element of an aligned group of four,
+    and at different ones."""
+    make_at = lambda k, t, sc: make(counts, t, 60 + k, 1, sc, head=heads[k])
+    g = make_at(0, dtype, 1.0)
+    p, m, v, ema, o = (make_at(k, "f32", sc) for k, sc in
+                       ((1, 0.1), (2, 0.02), (3, 0.1), (4, 0.1), (5, 1.0)))
+    for t in v:
+        t.square_()
+    before = [f64(x) for x in (g, p, m, v, ema)]
+    n = norm64(before[0])
+    lst = Parameters(g, p, m, v, ema=ema, clipped=o)
+    assert abs(float(lst.grad_norm()) - n) <= 2.0 ** -23 * n
+    assert abs(float(lst.clip(0.5)) - n) <= 2.0 ** -23 * n
+    assert np.all(np.abs(f64(o) - before[0] * 0.5 / n) <= np.abs(before[0] * 0.5 / n) * 2.0 ** -22 +
+                  2.0 ** -149)
+    lst.adamw(1.6e-3, (0.9, 0.99), 1e-8, 0.01, max_norm=0.5, ema_decay=0.99)
+    want = adamw64(*before, 1, 1.6e-3, (0.9, 0.99), 1e-8, 0.01, 0.5 / n, 0.99)
+    for (w, err), x in zip(want, (m, v, p, ema)):
+        off = np.abs(f64(x) - w) - err - 2.0 ** -148
+        assert off.max() <= 0, float(off.max())
+    assert np.array_equal(f64(g), before[0])
+
+
 def test_adamw_from_the_start(gpu):
     """Zero moments, step 0: the first update has the size lr wherever g is not 0."""
     g = make([300, 5], "f32", 13)

@@ -187,6 +187,8 @@ def test_kept_training_refuses(lib):
     assert size(m, e, 2, f, steps, None) == 0
     assert size(m, _Extent(1, 7, 8), 2, f, steps, good) == 0
     assert size(ctypes.byref(_Model(2, 16, 64, 3, 1)), e, 2, f, steps, good) == 0
+    big = _Extent(1, 1 << 18, 1 << 18)       # 2^36 cells, 2^31 - 1 steps: more than 2^64 bytes
+    assert size(m, big, 1, f, (ctypes.c_int32 * 1)(2 ** 31 - 1), good) == 0
     ws = (_LevelWeights * 2)(*[_LevelWeights(A, A, A, A, A)] * 2)
     gs = (_LevelGrads * 2)(*[_LevelGrads(A, A, A, A, A)] * 2)
     step = lib.octree_nca_train_step_kept
