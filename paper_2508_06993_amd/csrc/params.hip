@@ -210,6 +210,7 @@ template <int T> __device__ __forceinline__ double block_sum(double s) {
 // all of them before finish(k, q), so that N loads of an array are in flight.
 template <int T, int N, typename Load, typename Finish>
 __device__ __forceinline__ void for_groups(const Chunk &c, int t, Load load, Finish finish) {
+    static_assert(kParamChunk / 4 % (N * T) == 0, "a full chunk is whole rounds of N T groups");
     if (!c.quads) return;
     const int inner = (c.first + 3) / 4, outer = c.end / 4;   // whole ones: inner .. outer - 1
     if (inner == 0 && outer == kParamChunk / 4) {             // a full chunk: no comparisons
