@@ -10,8 +10,8 @@
 // the block's maxima and its codes (one read instead of two), the maxima are
 // unsigned maxima of the magnitudes' bits (a comparison for finite values only
 // where a block has others), one lane per channel divides, the slot list is on its
-// way with the values, and calls larger than the last-level cache go past it.  Small calls are bound by their launches: a
-// 320 x 320 state 4.1 us each way.
+// way with the values, and calls larger than the last-level cache go past it.
+// Small calls are bound by their launches: a 320 x 320 state 4.2 us each way.
 #include <algorithm>
 #include <type_traits>
 
