@@ -10,6 +10,7 @@ missing, every call raises ``OctreeNCAError``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -31,8 +32,8 @@ __all__ = [
     "octree_nca_step_backward_workspace_bytes", "octree_nca_step_backward",
     "octree_nca_upsample_backward", "octree_nca_readout_mse_workspace_bytes",
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
-    "level_grads_struct", "StateCacheBuffers", "state_cache_refs", "octree_nca_state_cache_write",
-    "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
+    "level_grads_struct", "check_train_weights", "StateCacheBuffers", "state_cache_refs",
+    "octree_nca_state_cache_write", "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
     "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
     "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
     "octree_nca_train_step_kept", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
@@ -559,12 +560,46 @@ def octree_nca_train_workspace_bytes(model: Model, finest, factors, steps) -> in
                                                       s))
 
 
+def _expect_elements(t, n: int, name: str) -> None:
+    if t.numel() != n:
+        raise OctreeNCAError(f"{name}: expected {n} elements, got {t.numel()}")
+
+
+def check_train_weights(model: Model, levels: int, weights, what="weights") -> None:
+    """Raises OctreeNCAError unless ``weights`` (or gradients) is a set per level,
+    each tensor of the model's size."""
+    if len(weights) != levels:
+        raise OctreeNCAError(f"{what}: {len(weights)} sets for {levels} levels")
+    c, h = model.channels, model.hidden
+    sizes = (("conv_w", c * 3 ** model.ndim), ("conv_b", c), ("w1", 2 * c * h), ("b1", h),
+             ("w2", c * h))
+    for lvl, w in enumerate(weights):
+        get = w.__getitem__ if isinstance(w, dict) else functools.partial(getattr, w)
+        for k, n in sizes:
+            _expect_elements(get(k), n, f"{what} {k} of level {lvl}")
+
+
+def _check_train(model: Model, levels: int, image, weights, target, grads, final_state) -> None:
+    """The library sees addresses only, and takes the sizes from the model and
+    the image's extent."""
+    d, h, w = image.shape[:3]
+    cells = d * h * w
+    _expect_elements(image, model.n_in * cells, "image")
+    _expect_elements(target, 2 * cells, "target")
+    if final_state is not None:
+        _expect_elements(final_state, model.channels * cells, "final_state")
+    check_train_weights(model, levels, weights)
+    check_train_weights(model, levels, grads, "grads")
+
+
 def octree_nca_train_step(model: Model, image, factors, weights, steps, fire_rate: float,
                           seed: int, target, workspace, grads, loss, final_state=None,
                           stream=None) -> None:
     """One training step; ``grads`` is a list (index = level) of gradient sets,
-    overwritten; ``loss`` a device float64 tensor of one element."""
+    overwritten; ``loss`` a device float64 tensor of one element; ``target`` is
+    [d][h][w][2].  Sizes that do not fit raise OctreeNCAError."""
     levels = len(steps)
+    _check_train(model, levels, image, weights, target, grads, final_state)
     d, h, w = image.shape[:3]
     ws = (_LevelWeights * levels)(*[level_weights_struct(x) for x in weights])
     gs = (_LevelGrads * levels)(*[level_grads_struct(x) for x in grads])
@@ -664,6 +699,7 @@ def octree_nca_train_step_kept(model: Model, image, factors, weights, steps, fir
                                code="i8", block=64, stream=None) -> None:
     """octree_nca_train_step with the states kept in 8 bits (``code``, ``block``)."""
     levels = len(steps)
+    _check_train(model, levels, image, weights, target, grads, final_state)
     d, h, w = image.shape[:3]
     ws = (_LevelWeights * levels)(*[level_weights_struct(x) for x in weights])
     gs = (_LevelGrads * levels)(*[level_grads_struct(x) for x in grads])

@@ -10,8 +10,8 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (Model, OctreeNCAError, StateCacheBuffers, octree_nca_adamw, octree_nca_clip_grads,
-               octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
+from . import (Model, OctreeNCAError, StateCacheBuffers, check_train_weights, octree_nca_adamw,
+               octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
                octree_nca_param_table_bytes, octree_nca_state_cache_read,
                octree_nca_state_cache_write, octree_nca_train_kept_workspace_bytes,
                octree_nca_train_step, octree_nca_train_step_kept,
@@ -167,6 +167,7 @@ class Trainer:
         self.finest = tuple(int(v) for v in finest)
         self.factors = [tuple(int(v) for v in f) for f in factors]
         self.steps = [int(v) for v in steps]
+        check_train_weights(model, len(self.steps), weights)
         device = weights[0]["w1"].device
         if keep is None:
             size = octree_nca_train_workspace_bytes(model, self.finest, self.factors, self.steps)
@@ -189,6 +190,9 @@ class Trainer:
     def gradients(self, image: torch.Tensor, target: torch.Tensor, fire_rate: float, seed: int,
                   final_state=None, stream=None) -> torch.Tensor:
         """Fills ``grads``; returns the loss (device fp64 [1], overwritten by the next call)."""
+        want = self.finest + (self.model.n_in,)
+        if tuple(image.shape) != want:
+            raise OctreeNCAError(f"image: expected {want}, got {tuple(image.shape)}")
         if self.keep is None:
             octree_nca_train_step(self.model, image, self.factors, self.weights, self.steps,
                                   fire_rate, seed, target, self.workspace, self.grads, self.loss,
