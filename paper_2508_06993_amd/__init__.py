@@ -33,8 +33,8 @@ __all__ = [
     "octree_nca_upsample_backward", "octree_nca_readout_mse_workspace_bytes",
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
     "level_grads_struct", "check_train_weights", "StateCacheBuffers", "state_cache_refs",
-    "octree_nca_state_cache_write", "octree_nca_state_cache_read", "param_structs", "octree_nca_param_table_bytes",
-    "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
+    "octree_nca_state_cache_write", "octree_nca_state_cache_read", "param_structs",
+    "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
     "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
     "octree_nca_train_step_kept", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
     "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
@@ -304,8 +304,13 @@ def _stream(stream) -> int:
     return int(stream)
 
 
-def _factors(factors: Sequence[Sequence[int]]):
+def _factors(factors: Sequence[Sequence[int]], levels: int):
+    """Array of three factors for each level but the coarsest; the library reads
+    that many."""
     flat = [int(v) for f in factors for v in f]
+    if len(flat) < 3 * (levels - 1):
+        raise OctreeNCAError(f"factors: {len(flat)} values for {levels} levels, expected "
+                             f"{3 * (levels - 1)}")
     arr = (_I32 * max(1, len(flat)))(*flat)
     return arr
 
@@ -344,7 +349,7 @@ def octree_nca_build_pyramid(model: Model, image: torch.Tensor, factors, level_i
                                        for t in level_images])
     st = lib().octree_nca_build_pyramid(ctypes.byref(model.struct()),
                                         _ptr(image, model.torch_dtype, "image"),
-                                        _extent((d, h, w)), levels, _factors(factors), imgs,
+                                        _extent((d, h, w)), levels, _factors(factors, levels), imgs,
                                         _stream(stream))
     _check(st, "octree_nca_build_pyramid")
 
@@ -396,7 +401,7 @@ def octree_nca_readout_classes(model: Model, state, classes: int, seg, stream=No
 def octree_nca_workspace_bytes(model: Model, finest, factors, with_final_state=True) -> int:
     levels = len(factors) + 1
     n = lib().octree_nca_workspace_bytes(ctypes.byref(model.struct()), _extent(finest), levels,
-                                         _factors(factors), 1 if with_final_state else 0)
+                                         _factors(factors, levels), 1 if with_final_state else 0)
     if n == 0:
         raise OctreeNCAError("octree_nca_workspace_bytes: invalid arguments", OCTNCA_EINVAL)
     return int(n)
@@ -409,7 +414,7 @@ def octree_nca_infer_launches(model: Model, finest, factors, steps) -> list:
     levels = len(factors) + 1
     out = (_I32 * levels)()
     st = lib().octree_nca_infer_launches(ctypes.byref(model.struct()), _extent(finest), levels,
-                                         _factors(factors), (_I32 * levels)(*steps), out)
+                                         _factors(factors, levels), (_I32 * levels)(*steps), out)
     _check(st, "octree_nca_infer_launches")
     return [int(v) for v in out]
 
@@ -426,7 +431,7 @@ def octree_nca_infer(model: Model, image, factors, weights, steps, fire_rate: fl
                                    for e in level_events])
     st = lib().octree_nca_infer(ctypes.byref(model.struct()),
                                 _ptr(image, model.torch_dtype, "image"), _extent((d, h, w)),
-                                levels, _factors(factors), ws,
+                                levels, _factors(factors, levels), ws,
                                 (_I32 * levels)(*[int(s) for s in steps]), float(fire_rate),
                                 int(seed), _ptr(workspace, torch.uint8, "workspace"),
                                 workspace.numel(),
@@ -445,7 +450,7 @@ def octree_nca_infer_static(model: Model, image, factors, weights, steps, fire_r
     ws = (_LevelWeights * levels)(*[level_weights_struct(x) for x in weights])
     st = lib().octree_nca_infer_static(ctypes.byref(model.struct()),
                                        _ptr(image, model.torch_dtype, "image"),
-                                       _extent((d, h, w)), levels, _factors(factors), ws,
+                                       _extent((d, h, w)), levels, _factors(factors, levels), ws,
                                        (_I32 * levels)(*[int(s) for s in steps]),
                                        float(fire_rate), int(seed),
                                        _ptr(final_state, model.torch_dtype, "final_state"),
@@ -463,7 +468,7 @@ def octree_nca_infer_batch(model: Model, images, factors, weights, steps, fire_r
     ws = (_LevelWeights * levels)(*[level_weights_struct(x) for x in weights])
     st = lib().octree_nca_infer_batch(ctypes.byref(model.struct()),
                                       _ptr(images, model.torch_dtype, "images"), int(batch),
-                                      _extent((d, h, w)), levels, _factors(factors), ws,
+                                      _extent((d, h, w)), levels, _factors(factors, levels), ws,
                                       (_I32 * levels)(*[int(s) for s in steps]),
                                       float(fire_rate), int(seed),
                                       _ptr(workspace, torch.uint8, "workspace"),
@@ -556,8 +561,8 @@ def octree_nca_train_workspace_bytes(model: Model, finest, factors, steps) -> in
     levels = len(steps)
     s = (_I32 * levels)(*[int(v) for v in steps])
     return int(lib().octree_nca_train_workspace_bytes(ctypes.byref(model.struct()),
-                                                      _extent(finest), levels, _factors(factors),
-                                                      s))
+                                                      _extent(finest), levels,
+                                                      _factors(factors, levels), s))
 
 
 def _expect_elements(t, n: int, name: str) -> None:
@@ -606,7 +611,7 @@ def octree_nca_train_step(model: Model, image, factors, weights, steps, fire_rat
     s = (_I32 * levels)(*[int(v) for v in steps])
     st = lib().octree_nca_train_step(
         ctypes.byref(model.struct()), _ptr(image, torch.float32, "image"), _extent((d, h, w)),
-        levels, _factors(factors), ws, s, float(fire_rate), int(seed),
+        levels, _factors(factors, levels), ws, s, float(fire_rate), int(seed),
         _ptr(target, torch.float32, "target"), _ptr(workspace, None, "workspace"),
         workspace.numel() * workspace.element_size(), gs, _ptr(loss, torch.float64, "loss"),
         _ptr(final_state, torch.float32, "final_state"), _stream(stream))
@@ -690,7 +695,7 @@ def octree_nca_train_kept_workspace_bytes(model: Model, finest, factors, steps, 
                                           block=64) -> int:
     levels = len(steps)
     return int(lib().octree_nca_train_kept_workspace_bytes(
-        ctypes.byref(model.struct()), _extent(finest), levels, _factors(factors),
+        ctypes.byref(model.struct()), _extent(finest), levels, _factors(factors, levels),
         (_I32 * levels)(*[int(v) for v in steps]), ctypes.byref(_keep(code, block))))
 
 
@@ -706,7 +711,7 @@ def octree_nca_train_step_kept(model: Model, image, factors, weights, steps, fir
     s = (_I32 * levels)(*[int(v) for v in steps])
     st = lib().octree_nca_train_step_kept(
         ctypes.byref(model.struct()), _ptr(image, torch.float32, "image"), _extent((d, h, w)),
-        levels, _factors(factors), ws, s, float(fire_rate), int(seed),
+        levels, _factors(factors, levels), ws, s, float(fire_rate), int(seed),
         _ptr(target, torch.float32, "target"), ctypes.byref(_keep(code, block)),
         _ptr(workspace, None, "workspace"), workspace.numel() * workspace.element_size(), gs,
         _ptr(loss, torch.float64, "loss"), _ptr(final_state, torch.float32, "final_state"),

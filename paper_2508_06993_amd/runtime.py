@@ -11,12 +11,11 @@ import numpy as np
 import torch
 
 from . import (Model, OctreeNCAError, StateCacheBuffers, check_train_weights, octree_nca_adamw,
-               octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer, octree_nca_param_table,
-               octree_nca_param_table_bytes, octree_nca_state_cache_read,
+               octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
+               octree_nca_param_table, octree_nca_param_table_bytes, octree_nca_state_cache_read,
                octree_nca_state_cache_write, octree_nca_train_kept_workspace_bytes,
-               octree_nca_train_step, octree_nca_train_step_kept,
-               octree_nca_train_workspace_bytes, octree_nca_workspace_bytes, param_structs,
-               state_cache_refs)
+               octree_nca_train_step, octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
+               octree_nca_workspace_bytes, param_structs, state_cache_refs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
 
