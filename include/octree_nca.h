@@ -460,7 +460,7 @@ typedef struct {
  *           of equal entries the last one's state is kept.
  * from is a multiple of block, and count too unless from + count = cells (a
  * long state may be written piece by piece).  n = 0 or count = 0 writes
- * nothing.  states must not overlap the cache.
+ * nothing.  states, slots and the cache must not overlap.
  * Errors: EINVAL, ESHAPE (a range outside the state or the cache), EUNSUPPORTED,
  * EHIP. */
 int octree_nca_state_cache_write(const octnca_model *model, const octnca_state_cache *cache,

@@ -34,8 +34,8 @@ __all__ = [
     "octree_nca_readout_mse", "octree_nca_train_workspace_bytes", "octree_nca_train_step",
     "level_grads_struct", "check_train_weights", "StateCacheBuffers", "state_cache_refs",
     "octree_nca_state_cache_write", "octree_nca_state_cache_read", "param_structs",
-    "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm", "octree_nca_clip_grads",
-    "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
+    "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm",
+    "octree_nca_clip_grads", "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
     "octree_nca_train_step_kept", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
     "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
     "OCTNCA_EUNSUPPORTED", "OCTNCA_ESHAPE",

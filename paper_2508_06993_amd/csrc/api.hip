@@ -1431,9 +1431,16 @@ int make_cache_args(const octnca_model *m, const octnca_state_cache *c, const vo
         return OCTNCA_EINVAL;
     if (count > kMaxCacheBytes / n / m->channels / 4) return OCTNCA_ESHAPE;
     const size_t state_bytes = (size_t)(count * n) * m->channels * elem_bytes(m);
-    if (overlap(states, state_bytes, c->codes, (size_t)(slot_bytes * c->slots)) ||
-        overlap(states, state_bytes, c->scales, (size_t)(4 * blocks * m->channels * c->slots)) ||
+    const size_t code_bytes = (size_t)(slot_bytes * c->slots);
+    const size_t scale_bytes = (size_t)(4 * blocks * m->channels * c->slots);
+    if (overlap(states, state_bytes, c->codes, code_bytes) ||
+        overlap(states, state_bytes, c->scales, scale_bytes) ||
         (slots && overlap(states, state_bytes, slots, (size_t)n * 8)))
+        return OCTNCA_EINVAL;
+    // a write's workgroups read the list while others write codes and scales
+    if (write && slots &&
+        (overlap(slots, (size_t)n * 8, c->codes, code_bytes) ||
+         overlap(slots, (size_t)n * 8, c->scales, scale_bytes)))
         return OCTNCA_EINVAL;
     a->codes = (int8_t *)c->codes;
     a->scales = c->scales;
