@@ -450,7 +450,7 @@ typedef struct {
     int64_t slots;  /* states the cache has room for, >= 0 */
     int64_t cells;  /* cells of one state, >= 1 */
     void *codes;    /* [slots][cells][C], one byte each; 4-byte aligned */
-    float *scales;  /* [slots][ceil(cells / block)][C]; 16-byte aligned */
+    float *scales;  /* [slots][ceil(cells / block)][C]; 16-byte aligned, outside codes */
 } octnca_state_cache;
 
 /* Quantises cells from .. from + count - 1 of n states into their slots:

@@ -1435,6 +1435,7 @@ int make_cache_args(const octnca_model *m, const octnca_state_cache *c, const vo
     const size_t scale_bytes = (size_t)(4 * blocks * m->channels * c->slots);
     if (overlap(states, state_bytes, c->codes, code_bytes) ||
         overlap(states, state_bytes, c->scales, scale_bytes) ||
+        overlap(c->codes, code_bytes, c->scales, scale_bytes) ||
         (slots && overlap(states, state_bytes, slots, (size_t)n * 8)))
         return OCTNCA_EINVAL;
     // a write's workgroups read the list while others write codes and scales

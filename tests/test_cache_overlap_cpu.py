@@ -23,3 +23,9 @@ def call(lib, write, slots=SLOTS, codes=CODES, scales=SCALES, n=4):
                                    SCALES + SCALE_BYTES - 8, SCALES - 8])
 def test_a_write_s_slot_list_lies_outside_the_cache(library_path, slots):
     assert call(octnca.lib(), True, slots) == EINVAL
+
+
+@pytest.mark.parametrize("write", [True, False])
+def test_codes_and_scales_lie_apart(library_path, write):
+    for scales in (CODES, CODES + CODE_BYTES - 16, CODES - SCALE_BYTES + 16):
+        assert call(octnca.lib(), write, scales=scales) == EINVAL
