@@ -299,6 +299,8 @@ def _stream(stream) -> int:
         # the current stream's handle; torch.cuda.current_stream() would also
         # make a Stream object, 2.7 us a call
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if type(stream) is int:
+        return stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)

@@ -4,14 +4,15 @@ and training.  Allocation and marshalling only; the computation is the library's
 """
 from __future__ import annotations
 
+import contextlib
 import warnings
 from typing import List, Optional, Sequence
 
 import numpy as np
 import torch
 
-from . import (Model, OctreeNCAError, StateCacheBuffers, check_train_weights, octree_nca_adamw,
-               octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
+from . import (Model, OctreeNCAError, StateCacheBuffers, _stream, check_train_weights,
+               octree_nca_adamw, octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
                octree_nca_param_table, octree_nca_param_table_bytes, octree_nca_state_cache_read,
                octree_nca_state_cache_write, octree_nca_train_kept_workspace_bytes,
                octree_nca_train_step, octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
@@ -70,10 +71,58 @@ def infer(model: Model, image: torch.Tensor, factors, weights, steps, fire_rate:
     return run(image, weights, steps, fire_rate, seed, stream=stream)
 
 
+def _on(stream):
+    """Context in which torch allocates and fills on ``stream`` (None: as it is)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
+
+
+class _Buffers:
+    """An object's own buffers, filled on the stream that is current here.  The
+    first use on another stream waits for the fills, and torch does not hand the
+    memory out again before that stream's work so far is done (a stream given as
+    a handle may be gone by then, so there the object has to outlive the work)."""
+
+    def __init__(self, *tensors):
+        self.tensors = tensors
+        self.streams = {_stream(None)}
+        # within a capture the graph has its own order
+        self.filled = None if torch.cuda.is_current_stream_capturing() else torch.cuda.Event()
+        if self.filled is not None:
+            self.filled.record()
+
+    def use(self, stream) -> int:
+        """Handle of the stream of a call."""
+        handle = _stream(stream)
+        if handle not in self.streams:
+            self._first_use(stream, handle)
+        return handle
+
+    def _first_use(self, stream, handle):
+        # a captured stream cannot wait for work outside; torch starts a capture
+        # with the device idle
+        if self.filled is None or torch.cuda.is_current_stream_capturing():
+            return
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        if isinstance(stream, torch.cuda.Stream):
+            stream.wait_event(self.filled)
+            for t in self.tensors:
+                t.record_stream(stream)
+        else:
+            torch.cuda.ExternalStream(handle).wait_event(self.filled)
+        self.streams.add(handle)
+
+
 class StateCache:
     """States of one model and extent held in 8 bits (octnca_state_cache):
     ``slots`` of them, each channel of ``block`` consecutive cells with one
-    scale.  ``codes`` / ``scales``: device memory to use instead of new."""
+    scale.  ``codes`` / ``scales``: device memory to use instead of new.  Calls
+    on any stream come after the fill of new memory; among each other they are
+    ordered by the caller, as is what else made the tensors they are given."""
 
     def __init__(self, model: Model, extent: Sequence[int], slots: int, code="i8", block=64,
                  codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
@@ -82,12 +131,16 @@ class StateCache:
         self.extent = tuple(int(v) for v in extent)
         d, h, w = self.extent
         cells, c = d * h * w, model.channels
+        own = []
         if codes is None:
             codes = torch.zeros((slots, cells, c), dtype=torch.int8, device=device)
+            own.append(codes)
         if scales is None:
             scales = torch.zeros((slots, -(-cells // block), c), device=device)
+            own.append(scales)
         self.buffers = StateCacheBuffers(codes, scales, cells, code, block)
         self.refs = state_cache_refs(model, self.buffers)
+        self._own = _Buffers(*own)
 
     def write(self, states: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0,
               from_cell=0, stream=None) -> None:
@@ -95,13 +148,13 @@ class StateCache:
         ``slots``: device int64 [n], entries outside the cache are left out; or
         None for slots first, first + 1, ..."""
         octree_nca_state_cache_write(self.model, self.buffers, states, from_cell, slots, first,
-                                     stream, self.refs)
+                                     self._own.use(stream), self.refs)
 
     def read(self, out: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0, from_cell=0,
              stream=None) -> torch.Tensor:
         """Fills and returns ``out`` [n][...][C]; slots outside the cache read as zeros."""
-        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first, stream,
-                                    self.refs)
+        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first,
+                                    self._own.use(stream), self.refs)
         return out
 
 
@@ -114,7 +167,8 @@ class Parameters:
     ``ema`` are fp32.  The tensors are read and written where they are: the list
     keeps them alive, and they must not be replaced by others.  ``step`` is the
     number of updates made so far (device int64 [1]).  Calls of one list must
-    not overlap (it holds their scratch memory)."""
+    not overlap (it holds their scratch memory).  ``stream`` is the one that the
+    list is made on; calls on any stream come after that."""
 
     def __init__(self, grads, params=None, m=None, v=None, ema=None, clipped=None,
                  step: Optional[torch.Tensor] = None, stream=None):
@@ -123,21 +177,27 @@ class Parameters:
         device = self.tensors[0][0].device if self.tensors[0] else torch.device("cuda")
         structs = param_structs(*self.tensors)
         n = len(self.tensors[0])
-        self.table = torch.empty(octree_nca_param_table_bytes(structs, n), dtype=torch.uint8,
-                                 device=device)
-        self.list = octree_nca_param_table(structs, n, self.table, stream)
-        self.norm = torch.zeros((), device=device)
-        self.step = step if step is not None else torch.zeros(1, dtype=torch.int64, device=device)
+        size = octree_nca_param_table_bytes(structs, n)
+        with _on(stream):
+            self.table = torch.empty(size, dtype=torch.uint8, device=device)
+            self.list = octree_nca_param_table(structs, n, self.table)
+            self.norm = torch.zeros((), device=device)
+            own = [self.table, self.norm]
+            if step is None:
+                step = torch.zeros(1, dtype=torch.int64, device=device)
+                own.append(step)
+            self.step = step
+            self._own = _Buffers(*own)
 
     def grad_norm(self, scale=1.0, stream=None) -> torch.Tensor:
         """scale * (2-norm of all gradients), a device scalar that the next call overwrites."""
-        octree_nca_grad_norm(self.list, self.norm, scale, stream)
+        octree_nca_grad_norm(self.list, self.norm, scale, self._own.use(stream))
         return self.norm
 
     def clip(self, max_norm: float, scale=1.0, stream=None) -> torch.Tensor:
         """clipped = scale * gradients, shortened to ``max_norm`` if their norm
         is larger; returns the norm (as grad_norm)."""
-        octree_nca_clip_grads(self.list, max_norm, scale, self.norm, stream)
+        octree_nca_clip_grads(self.list, max_norm, scale, self.norm, self._own.use(stream))
         return self.norm
 
     def adamw(self, lr: float, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0,
@@ -145,7 +205,7 @@ class Parameters:
         """One update with the clipped gradients; left out if their norm is not
         finite.  Returns the norm before clipping (as grad_norm)."""
         octree_nca_adamw(self.list, self.step, lr, betas, eps, weight_decay, max_norm, scale,
-                         ema_decay, self.norm, stream)
+                         ema_decay, self.norm, self._own.use(stream))
         return self.norm
 
 
@@ -157,7 +217,8 @@ class Trainer:
     updated in place; ``ema`` their running averages.  ``keep``: None keeps every
     state in fp32 (octree_nca_train_step), "i8" or "f8" in 8 bits
     (octree_nca_train_step_kept), in about half the memory at 20 steps a level
-    and less with more steps."""
+    and less with more steps.  Steps on any stream come after what the
+    constructor enqueued; steps on several streams are ordered by the caller."""
 
     def __init__(self, model: Model, finest: Sequence[int], factors, steps, weights,
                  keep: Optional[str] = None, block=64, lr=1.6e-3, betas=(0.9, 0.99), eps=1e-8,
@@ -180,11 +241,13 @@ class Trainer:
         self.grads, self.ema = like(torch.zeros_like), like(torch.clone)
         m, v = like(torch.zeros_like), like(torch.zeros_like)
         flat = lambda sets: [s[k] for s in sets for k in WEIGHT_FIELDS]
+        self.loss = torch.zeros(1, dtype=torch.float64, device=device)
+        self._own = _Buffers(self.workspace, self.loss,
+                             *(t for sets in (self.grads, self.ema, m, v) for t in flat(sets)))
         self.parameters = Parameters(flat(self.grads), flat(weights), flat(m), flat(v),
                                      ema=flat(self.ema))
         self.settings = dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
                              max_norm=max_norm, ema_decay=ema_decay)
-        self.loss = torch.zeros(1, dtype=torch.float64, device=device)
 
     def gradients(self, image: torch.Tensor, target: torch.Tensor, fire_rate: float, seed: int,
                   final_state=None, stream=None) -> torch.Tensor:
@@ -192,6 +255,7 @@ class Trainer:
         want = self.finest + (self.model.n_in,)
         if tuple(image.shape) != want:
             raise OctreeNCAError(f"image: expected {want}, got {tuple(image.shape)}")
+        stream = self._own.use(stream)
         if self.keep is None:
             octree_nca_train_step(self.model, image, self.factors, self.weights, self.steps,
                                   fire_rate, seed, target, self.workspace, self.grads, self.loss,
