@@ -548,16 +548,17 @@ size_t octree_nca_param_table_bytes(const octnca_param *params, int32_t n);
 int octree_nca_param_table(const octnca_param *params, int32_t n, void *table, size_t table_bytes,
                            octnca_param_list *list, void *stream);
 
-/* *norm (device) = scale * sqrt(sum over all gradients of g^2), summed in fp64.
+/* *norm (device) = scale * sqrt(sum over all gradients of g^2), summed in fp64
+ * and rounded to fp32 (infinite past its range).
  * scale > 0 and finite (the inverse of a loss scale, or of a batch's size).
  * The norm of no elements is 0.  Errors: EINVAL, EHIP. */
 int octree_nca_grad_norm(const octnca_param_list *list, float scale, float *norm, void *stream);
 
 /* clipped = grad * f with f = scale if norm <= max_norm, else scale * max_norm /
- * norm, for the norm of octree_nca_grad_norm: f is rounded to fp32 once, the
- * product once to clipped's type.  A gradient that is not finite shows: with an
- * infinite norm the infinite ones become NaN and the others 0, with a NaN norm
- * all become NaN (max_norm finite).
+ * norm, for the norm of octree_nca_grad_norm before its rounding: f is rounded to
+ * fp32 once, the product once to clipped's type.  A gradient that is not finite
+ * shows: if one is NaN all become NaN, else if one is infinite the infinite ones
+ * become NaN and the others 0 (max_norm finite).
  *   max_norm  > 0, may be infinite (no clipping);
  *   norm      device fp32 or NULL: receives the norm.
  * Errors: EINVAL (also a list without `clipped`), EHIP. */
@@ -582,8 +583,8 @@ typedef struct {
  *                + weight_decay param);
  *   ema = ema_decay ema + (1 - ema_decay) param   (lists with ema);
  *   *step = t.
- * Where the norm is not finite nothing of this is written (*norm still is), as
- * a step with an overflowed gradient is left out.
+ * Where the norm is not finite in fp32 nothing of this is written (*norm still
+ * is), as a step with an overflowed gradient is left out.
  *   step  device int64: updates made so far, >= 0;
  *   norm  device fp32 or NULL: receives the norm before clipping.
  * The gradients are not changed.  Errors: EINVAL, EHIP. */

@@ -386,6 +386,9 @@ struct UpdateArgs {
     float lr, beta1, beta2, rest1, rest2, eps, decay, ema, ema_rest;
 };
 
+// Whether an update is made: by the norm as the caller sees it, in fp32.
+__device__ __forceinline__ bool norm_fits(double len) { return __builtin_isfinite((float)len); }
+
 // One element: g already clipped; corr = 1 / (1 - beta^t).
 __device__ __forceinline__ void update(const UpdateArgs &u, float corr1, float corr2, float g,
                                        float &p, float &m, float &v) {
@@ -465,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void adamw(const Scratch *scratch, int su
         STREAM ? sqrt(scratch->total) * u.scale : norm_of(scratch, sums, u.scale);
     const bool first = blockIdx.x == 0 && threadIdx.x == 0;
     if (norm && first) *norm = (float)len;
-    if (!__builtin_isfinite(len)) return;
+    if (!norm_fits(len)) return;
     if (first) *step += 1;
     const float f = clip_factor(len, u.scale, u.max_norm);
     const float corr1 = (float)scratch->corr1, corr2 = (float)scratch->corr2;
@@ -549,7 +552,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_adamw(Scratch *scratch, c
         Group<DT, false> own;
         if (whole) own.load(c, q);
         const double len = small_norm(chunks, n, u.scale);
-        const bool fine = __builtin_isfinite(len);
+        const bool fine = norm_fits(len);
         const int64_t t = now;
         if (threadIdx.x == 0) {
             if (norm && blockIdx.x == 0) *norm = (float)len;
