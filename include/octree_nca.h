@@ -565,7 +565,8 @@ int octree_nca_grad_norm(const octnca_param_list *list, float scale, float *norm
 int octree_nca_clip_grads(const octnca_param_list *list, float scale, float max_norm, float *norm,
                           void *stream);
 
-/* Settings of one AdamW update (decoupled weight decay). */
+/* Settings of one AdamW update (decoupled weight decay).  lr, eps, weight_decay
+ * and scale are in these ranges, and finite, once rounded to fp32. */
 typedef struct {
     double lr;            /* >= 0 */
     double beta1, beta2;  /* in [0, 1) */

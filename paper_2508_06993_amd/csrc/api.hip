@@ -1619,9 +1619,10 @@ int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings
         return OCTNCA_EINVAL;
     const octnca_adamw &h = *settings;
     auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
-    auto not_negative = [](double x) { return x >= 0.0 && x < HUGE_VAL; };
+    // the kernels use these in fp32
+    auto not_negative = [](double x) { return x >= 0.0 && (float)x < HUGE_VALF; };
     if (!not_negative(h.lr) || !beta_ok(h.beta1) || !beta_ok(h.beta2) || !positive((float)h.eps) ||
-        !not_negative(h.weight_decay) || !(h.max_norm > 0.0) || !positive(h.scale) ||
+        !not_negative(h.weight_decay) || !(h.max_norm > 0.0) || !positive((float)h.scale) ||
         !(h.ema_decay >= 0.0 && h.ema_decay <= 1.0))
         return OCTNCA_EINVAL;
     return hip_status(launch_adamw(*list, h, step, norm, (hipStream_t)stream));
