@@ -736,8 +736,6 @@ def _grad_type(t, name):
 
 def _addresses(tensors, counts, device, dtype, name):
     """Addresses of a list of contiguous device tensors of the given sizes."""
-    if len(tensors) != len(counts):
-        raise OctreeNCAError(f"{name}: {len(tensors)} tensors for {len(counts)} gradients")
     out = [_ptr(t, dtype, name) for t in tensors]
     for t, n in zip(tensors, counts):
         if t.numel() != n:
@@ -749,6 +747,9 @@ def _addresses(tensors, counts, device, dtype, name):
 
 def param_structs(grads, params=None, m=None, v=None, ema=None, clipped=None):
     """Array of octnca_param for lists of device tensors (index = tensor)."""
+    for k, x in (("param", params), ("m", m), ("v", v), ("ema", ema), ("clipped", clipped)):
+        if x is not None and len(x) != len(grads):
+            raise OctreeNCAError(f"{k}: {len(x)} tensors for {len(grads)} gradients")
     if not grads:
         return (_Param * 1)()
     counts = [g.numel() for g in grads]
