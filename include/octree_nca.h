@@ -440,7 +440,9 @@ int octree_nca_train_step(const octnca_model *model, const void *image, octnca_e
  *     its NaN stands for a value that is not finite.
  * Reading gives code * scale, computed in fp32 and rounded to the state's
  * storage type; a value that was not finite reads back as NaN and leaves the
- * others of its block as they are.
+ * others of its block as they are.  Finite values at the end of the type's range
+ * whose codes round past it read back as infinities: with OCTNCA_CODE_F8 from
+ * 31/32 of 2^16 (fp16) or 2^128 (fp32) on, with OCTNCA_CODE_I8 fp32's largest.
  * ------------------------------------------------------------------------- */
 typedef enum { OCTNCA_CODE_I8 = 0, OCTNCA_CODE_F8 = 1 } octnca_code;
 
@@ -460,9 +462,10 @@ typedef struct {
  *           of equal entries the last one's state is kept.
  * from is a multiple of block, and count too unless from + count = cells (a
  * long state may be written piece by piece).  n = 0 or count = 0 writes
- * nothing.  states, slots and the cache must not overlap.
- * Errors: EINVAL, ESHAPE (a range outside the state or the cache), EUNSUPPORTED,
- * EHIP. */
+ * nothing.  states, slots and the cache must not overlap.  Each state's part of a
+ * call looks through the entries of `slots` after its own (n^2 / 2 of them in all).
+ * Errors: EINVAL, ESHAPE (a range outside the state or the cache, 2^31 - 2^17
+ * states or more), EUNSUPPORTED, EHIP. */
 int octree_nca_state_cache_write(const octnca_model *model, const octnca_state_cache *cache,
                                  const void *states, int64_t from, int64_t count, int32_t n,
                                  const int64_t *slots, int64_t first, void *stream);

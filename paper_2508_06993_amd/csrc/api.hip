@@ -24,6 +24,7 @@ constexpr int64_t kMaxDim = int64_t(1) << 30;      // per axis (kernels index wi
 constexpr int64_t kMaxCells = int64_t(1) << 36;    // per level
 constexpr int kMaxLevels = 16;
 constexpr int64_t kMaxCacheBytes = int64_t(1) << 60;
+constexpr int32_t kMaxCacheStates = INT32_MAX - (1 << 17);   // of a call (steps of int past them)
 constexpr int kMaxGroup = 64;   // images of a batch that run together at most
 constexpr size_t kAlign = 256;
 
@@ -1409,6 +1410,7 @@ int make_cache_args(const octnca_model *m, const octnca_state_cache *c, const vo
     const int st = check_model(m);
     if (st) return st;
     if (c == nullptr || n < 0 || from < 0 || count < 0) return OCTNCA_EINVAL;
+    if (n > kMaxCacheStates) return OCTNCA_ESHAPE;
     if (c->code != OCTNCA_CODE_I8 && c->code != OCTNCA_CODE_F8) return OCTNCA_EINVAL;
     if (c->block != 32 && c->block != 64 && c->block != 128) return OCTNCA_EINVAL;
     if (c->slots < 0 || c->cells < 1 || c->cells > kMaxCells) return OCTNCA_ESHAPE;
