@@ -294,13 +294,17 @@ def _ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     return t.data_ptr()
 
 
+# the current stream's handle comes from these; torch.cuda.current_stream() would
+# also make a Stream object, 2.7 us a call
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
-    if stream is None:
-        # the current stream's handle; torch.cuda.current_stream() would also
-        # make a Stream object, 2.7 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if type(stream) is int:
         return stream
+    if stream is None:
+        return _current_handle(_current_device())
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
@@ -583,7 +587,8 @@ def check_train_weights(model: Model, levels: int, weights, what="weights") -> N
     for lvl, w in enumerate(weights):
         get = w.__getitem__ if isinstance(w, dict) else functools.partial(getattr, w)
         for k, n in sizes:
-            _expect_elements(get(k), n, f"{what} {k} of level {lvl}")
+            if get(k).numel() != n:
+                _expect_elements(get(k), n, f"{what} {k} of level {lvl}")
 
 
 def _check_train(model: Model, levels: int, image, weights, target, grads, final_state) -> None:
@@ -653,18 +658,20 @@ class StateCacheBuffers:
                            _ptr(self.scales, torch.float32, "scales"))
 
 
-def _cache_call(name, model, refs, states, from_cell, slots, first, stream):
-    """states: [n][cells...][C]; refs: the model's and the cache's structs by reference."""
+def _cache_call(call, model, refs, states, from_cell, slots, first, stream):
+    """A state-cache call (a function of lib()): states [n][cells...][C], refs of
+    state_cache_refs."""
     shape = states.shape
     n, c = shape[0], shape[-1]
     if c != model.channels:
         raise OctreeNCAError(f"states: expected {model.channels} channels, got {c}")
     if slots is not None and slots.shape != (n,):
         raise OctreeNCAError(f"slots: expected shape {(n,)}, got {tuple(slots.shape)}")
-    st = getattr(lib(), name)(*refs, _ptr(states, model.torch_dtype, "states"), from_cell,
-                              states.numel() // (n * c) if n else 0, n,
-                              _ptr(slots, torch.int64, "slots"), first, _stream(stream))
-    _check(st, name)
+    st = call(*refs, _ptr(states, model.torch_dtype, "states"), from_cell,
+              states.numel() // (n * c) if n else 0, n, _ptr(slots, torch.int64, "slots"), first,
+              _stream(stream))
+    if st:
+        _check(st, call.__name__)
 
 
 def state_cache_refs(model: Model, cache: StateCacheBuffers):
@@ -676,14 +683,14 @@ def octree_nca_state_cache_write(model: Model, cache: StateCacheBuffers, states,
                                  slots=None, first=0, stream=None, refs=None) -> None:
     """Quantise states [n][...cells][C] into the slots ``slots`` (device int64
     [n]) or first, first + 1, ..."""
-    _cache_call("octree_nca_state_cache_write", model, refs or state_cache_refs(model, cache),
+    _cache_call(lib().octree_nca_state_cache_write, model, refs or state_cache_refs(model, cache),
                 states, from_cell, slots, first, stream)
 
 
 def octree_nca_state_cache_read(model: Model, cache: StateCacheBuffers, states, from_cell=0,
                                 slots=None, first=0, stream=None, refs=None) -> None:
     """Fill states [n][...cells][C] with the values of the slots."""
-    _cache_call("octree_nca_state_cache_read", model, refs or state_cache_refs(model, cache),
+    _cache_call(lib().octree_nca_state_cache_read, model, refs or state_cache_refs(model, cache),
                 states, from_cell, slots, first, stream)
 
 

@@ -11,11 +11,11 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (Model, OctreeNCAError, StateCacheBuffers, _stream, check_train_weights,
-               octree_nca_adamw, octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
-               octree_nca_param_table, octree_nca_param_table_bytes, octree_nca_state_cache_read,
-               octree_nca_state_cache_write, octree_nca_train_kept_workspace_bytes,
-               octree_nca_train_step, octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
+from . import (Model, OctreeNCAError, StateCacheBuffers, _stream, _cache_call, check_train_weights,
+               lib, octree_nca_adamw, octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
+               octree_nca_param_table, octree_nca_param_table_bytes,
+               octree_nca_train_kept_workspace_bytes, octree_nca_train_step,
+               octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
                octree_nca_workspace_bytes, param_structs, state_cache_refs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
@@ -147,14 +147,14 @@ class StateCache:
         """states [n][...][C]: whole states, or their cells from ``from_cell`` on.
         ``slots``: device int64 [n], entries outside the cache are left out; or
         None for slots first, first + 1, ..."""
-        octree_nca_state_cache_write(self.model, self.buffers, states, from_cell, slots, first,
-                                     self._own.use(stream), self.refs)
+        _cache_call(lib().octree_nca_state_cache_write, self.model, self.refs, states, from_cell,
+                    slots, first, self._own.use(stream))
 
     def read(self, out: torch.Tensor, slots: Optional[torch.Tensor] = None, first=0, from_cell=0,
              stream=None) -> torch.Tensor:
         """Fills and returns ``out`` [n][...][C]; slots outside the cache read as zeros."""
-        octree_nca_state_cache_read(self.model, self.buffers, out, from_cell, slots, first,
-                                    self._own.use(stream), self.refs)
+        _cache_call(lib().octree_nca_state_cache_read, self.model, self.refs, out, from_cell, slots,
+                    first, self._own.use(stream))
         return out
 
 
