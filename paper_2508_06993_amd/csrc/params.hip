@@ -574,12 +574,18 @@ __global__ __launch_bounds__(kSmallThreads) void small_adamw(Scratch *scratch, c
     });
 }
 
-// Lists that take one launch, calls in a row (one launch, two): of 25 tensors
-// and 16.5k elements an update 6.5 and 7.4-8.7 us, clipping 4.7 and 6.8-8.1, the
-// norm 4.0 and 6.6-7.5; of 50 tensors and 33k elements 8.3 and 7.5-8.8, 6.3 and
-// 6.8-8.2, 5.1 and 6.6-7.6; of twice that 12.3 and 7.5-8.7, 9.6 and 6.8-8.3.
+// Lists that take one launch.  Calls in a row take two launches 7.2 to 9.0 us for an
+// update, 6.4 to 8.7 for clipping, 6.3 to 7.9 for the norm (by the machine, hardly by
+// the list).  One launch:
+//   25 tensors of 656 elements   6.8   4.7   3.8 to 4.3
+//   37                           7.4   5.3   4.2 to 4.4
+//   50                           8.5   6.3   5.1
+//   75                          10.2   7.6   6.5
+// and, as every workgroup goes through all chunks, of any size,
+//   64 tensors of 16 elements    9.4   7.0   5.9
+//   128 of 16, or of 192        14.3  11.2  10.2
 constexpr int64_t kSmallUpdate = 3 << 13, kSmallNorm = 1 << 15;   // elements
-constexpr int64_t kSmallChunks = 128;
+constexpr int64_t kSmallChunks = 64;
 bool small(const octnca_param_list &l, int64_t elements) {
     return l.elements <= elements && l.chunks <= kSmallChunks;
 }
