@@ -6,7 +6,7 @@
 // Every element depends on all gradients through the norm, so a call is two
 // passes: squares (in fp64, added in an order that does not depend on the run),
 // then the elements.  Both are bound by memory: 250M bf16 gradients into bf16
-// 86 + 162 us (5.8 and 6.2 TB/s), 30M packed fp32 ones 21 + 40 us, an update of
+// 86 + 168 us (5.8 and 6.0 TB/s), 30M packed fp32 ones 21 + 40 us, an update of
 // 100M elements with bf16 gradients and a running average 35 + 5 + 568 us (3.4
 // GB, 6.0 TB/s).  Reading alone reaches 6.3 TB/s on this card, a large copy 4.4
 // to 5.1.  Small lists are bound by launches and take one (see kSmallUpdate):
@@ -591,8 +591,12 @@ bool small(const octnca_param_list &l, int64_t elements) {
 }
 unsigned small_grid(const octnca_param_list &l) { return (unsigned)std::max<int64_t>(1, l.chunks); }
 
-// Lists whose arrays pass the last-level cache of 256 MB before the next call:
-// the second pass then goes past it.
+// Lists whose second pass goes past the last-level cache (256 MB), from half its size
+// on: the next call finds little of them there.  us past it and through it, of one
+// list again and again (of three in turn), by the bytes of the arrays: clipping of
+// 128 MB 31 and 34 (31, 38), 256 MB 57 and 59 (57, 74), 512 MB 114 and 144 (117, 148);
+// an update, which then also has a workgroup per chunk, of 96 MB 23 and 21 (24, 22),
+// 128 MB 28 and 28 (30, 28), 192 MB 39 and 39 (40, 45), 1 GB 181 and 219 (178, 222).
 bool streams(const octnca_param_list &l) { return l.bytes >= (int64_t(1) << 27); }
 
 // Enqueues the first pass; the number of sums it leaves.
@@ -686,8 +690,8 @@ hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64
     }
     const int sums = first_pass(l, step, h.beta1, h.beta2, stream);
     if (streams(l)) {
-        // A workgroup per chunk: 100M elements 577 us, with 2048 workgroups that
-        // loop over the chunks 617.  So many do not each add the sums.
+        // A workgroup per chunk: a call of 100M elements takes 635 us, with 2048
+        // workgroups that loop over the chunks 765.  So many do not each add the sums.
         add_sums<<<1, kThreads, 0, stream>>>(scratch_of(l.table), sums);
         adamw<true><<<(unsigned)std::min(l.chunks, kMaxGrid), kThreads, 0, stream>>>(
             scratch_of(l.table), sums, chunks_of(l.table), l.chunks, u, step, norm);

@@ -4,14 +4,14 @@
 // Both directions are one pass over memory: a write reads a value once and
 // leaves one byte of it, a read the reverse, and a block's scales add 4 bytes per
 // channel.  A 184.5M-cell fp32 state (11.8 GB, blocks of 64) is written in 2.43
-// ms and read back in 2.49 ms, 6.1 TB/s of these bytes each (counters show no
+// ms and read back in 2.49 ms, 6.2 and 6.0 TB/s of these bytes (counters show no
 // others); a copy of 8 GB reaches 4.4 TB/s on this card and reading alone 6.3.
 // What took the writes there from 3.0 TB/s: the values stay in registers between
 // the block's maxima and its codes (one read instead of two), the maxima are
 // unsigned maxima of the magnitudes' bits (a comparison for finite values only
 // where a block has others), one lane per channel divides, the slot list is on its
 // way with the values, and calls larger than the last-level cache go past it.
-// Small calls are bound by their launches: a 320 x 320 state 4.2 us each way.
+// Small calls are bound by their launches: a 320 x 320 state 4.5 and 4.3 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_write(CacheArgs a, uint32_t
 
 // A thread takes channel quads of a state, the workgroup's threads apart: 32
 // bytes of the state's values (of one quad a thread fp16 states were read at 3.0
-// TB/s, of four at 5.5).  The workgroups do not loop: a grid of 2048 that loop
+// TB/s, of four at 5.8).  The workgroups do not loop: a grid of 2048 that loop
 // over a 184.5M-cell state took 3.1 ms instead of 2.5.
 template <typename T> constexpr int kReadQuads = sizeof(T) == 4 ? 2 : 4;
 template <typename T, int C, typename Code>
@@ -441,8 +441,11 @@ hipError_t run_write(const CacheArgs &a, const void *states, hipStream_t stream)
 
 template <typename T, int C, typename Code>
 hipError_t run(CacheArgs a, bool write, void *states, hipStream_t stream) {
-    // past this size nothing of the call is still in the last-level cache (256 MB)
-    // when it is wanted next
+    // Past the last-level cache (256 MB) from half its size on: what is wanted next
+    // is little of a call of this size.  us past it and through it, of one state
+    // again and again (of three in turn): writes of 96 MB 16 and 15 (17, 16), 128 MB
+    // 21 and 20 (22, 24), 256 MB 42 and 36 (42, 46), 512 MB 83 and 91 (84, 91); reads
+    // of 128 MB 25 and 20 (25, 27), 256 MB 44 and 37 (47, 47), 1 GB 177 and 175.
     a.stream = a.count * a.n * C * (int64_t)(sizeof(T) + 1) >= int64_t(1) << 27;
     if (!write) {
         const int64_t per = kReadQuads<T> * 64 * kWaves;
