@@ -11,7 +11,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence

@@ -71,13 +71,18 @@ def infer(model: Model, image: torch.Tensor, factors, weights, steps, fire_rate:
     return run(image, weights, steps, fire_rate, seed, stream=stream)
 
 
+def _torch_stream(stream):
+    """torch's stream of a stream or a handle (0: the default stream)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(stream)) if stream else torch.cuda.default_stream()
+
+
 def _on(stream):
     """Context in which torch allocates and fills on ``stream`` (None: as it is)."""
     if stream is None:
         return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
-    return torch.cuda.stream(stream)
+    return torch.cuda.stream(_torch_stream(stream))
 
 
 class _Buffers:
@@ -108,12 +113,10 @@ class _Buffers:
             return
         if stream is None:
             stream = torch.cuda.current_stream()
+        _torch_stream(stream).wait_event(self.filled)
         if isinstance(stream, torch.cuda.Stream):
-            stream.wait_event(self.filled)
             for t in self.tensors:
                 t.record_stream(stream)
-        else:
-            torch.cuda.ExternalStream(handle).wait_event(self.filled)
         self.streams.add(handle)
 
 

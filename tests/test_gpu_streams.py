@@ -131,3 +131,24 @@ def test_memory_of_a_list_that_is_gone(gpu):
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("made_on_it", [False, True])
+def test_the_default_stream_by_its_handle(gpu, made_on_it):
+    """Handle 0 is the default stream, also where another one is current."""
+    want = lists(COUNTS)
+    Parameters(*want).adamw(0.01, max_norm=1.0)
+    got = lists(COUNTS)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        keep_busy()
+        p = Parameters(*got, stream=0) if made_on_it else Parameters(*got)
+        p.adamw(0.01, max_norm=1.0, stream=0)
+        if made_on_it:      # nothing here has waited for the busy stream
+            torch.cuda.default_stream().synchronize()
+            assert not side.query()
+    torch.cuda.synchronize()
+    assert int(p.step) == 1
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
