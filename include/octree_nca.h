@@ -595,6 +595,117 @@ typedef struct {
 int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings, int64_t *step,
                      float *norm, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Cell layers: linear layers on every cell (a head on a state's channels, a
+ * layer of it), with weights and kept inputs in microscaled 4 bits, and dropout
+ * whose mask is never stored.
+ *
+ * Rows are cells, columns channels.  A matrix in 4 bits has a scale for every
+ * block of 32 consecutive columns of a row (the last block may have fewer):
+ *   a = max |x| of the block, s = the smallest power of two >= 2^-127 with
+ *   a <= 6 s, code = x / s rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6
+ *   and their negatives (ties to the even code; sign bit, 2 exponent bits, 1
+ *   mantissa bit).  No value saturates: the error is at most half a step.
+ * A block with a value that is not finite has no scale: all of it stands for NaN.
+ * The value of a code is code * s.
+ * ------------------------------------------------------------------------- */
+
+/* A matrix of values: row r starts at data + r * stride elements, its columns lie
+ * one after the other.  data is aligned to its type; stride >= columns (any
+ * value, if there is one row). */
+typedef struct {
+    void *data;
+    int64_t stride;
+    int32_t dtype;   /* octnca_dtype */
+} octnca_rows;
+
+/* A matrix in 4 bits.  With B = ceil(cols / 32), block b of row r has its codes at
+ *   codes + (((r / 16) * B + b) * 16 + r % 16) * 16, 16 bytes, the first column in
+ * the lowest four bits, columns past the last being 0, and its scale at
+ *   scales + ((r / 16) * B + b) * 16 + r % 16, one byte: s = 2^(byte - 127), 255 NaN.
+ * Rows from `rows` on up to the next multiple of 16 take up space; no call
+ * writes them and no result depends on them. */
+typedef struct {
+    int64_t rows;    /* >= 0 */
+    int64_t cols;    /* 1 .. 2^20 */
+    void *codes;     /* octree_nca_mx4_code_bytes; 16-byte aligned */
+    void *scales;    /* 1/16 of that; 16-byte aligned, outside codes */
+} octnca_mx4;
+
+/* Bytes of codes of a matrix, 256 * ceil(rows / 16) * ceil(cols / 32) (0 if there
+ * are no rows or the size is invalid). */
+size_t octree_nca_mx4_code_bytes(int64_t rows, int64_t cols);
+
+/* m = x in 4 bits.  x [m->rows][m->cols], fp32, fp16 or bf16, outside m.
+ * Errors: EINVAL, ESHAPE, EHIP. */
+int octree_nca_mx4_quantise(const octnca_rows *x, const octnca_mx4 *m, void *stream);
+
+/* x = the values of m, rounded once to x's type (fp16 past its range: infinite). */
+int octree_nca_mx4_dequantise(const octnca_mx4 *m, const octnca_rows *x, void *stream);
+
+/* out[r][n] = sum over k of a[r][k] w[n][k] + bias[n], summed in fp32 and rounded
+ * once to out's type; with relu, what is below 0 becomes 0 (NaN stays).
+ *   a     [rows][cols];  w [outs][cols], the weights;
+ *   bias  device fp32 [outs], or NULL;
+ *   out   [rows][outs], fp32, fp16 or bf16; outside the other arrays.
+ * The order of the sums depends on the sizes only.  Errors: EINVAL, ESHAPE, EHIP. */
+int octree_nca_mx4_product(const octnca_mx4 *a, const octnca_mx4 *w, const float *bias,
+                           int32_t relu, const octnca_rows *out, void *stream);
+
+/* octree_nca_mx4_quantise of x into kept, then octree_nca_mx4_product of kept and
+ * w (the same codes; sums of a few rows may be taken in another order).  kept is
+ * what the layer's backward reads. */
+int octree_nca_mx4_linear(const octnca_rows *x, const octnca_mx4 *kept, const octnca_mx4 *w,
+                          const float *bias, int32_t relu, const octnca_rows *out, void *stream);
+
+/* Bytes of workspace octree_nca_mx4_backward needs (0 if a size is invalid). */
+size_t octree_nca_mx4_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t outs);
+
+/* Gradients of octree_nca_mx4_product without its relu, for the gradient G of out
+ * (straight through the rounding to 4 bits):
+ *   grad_in[r][k]     = sum over n of G[r][n] w[n][k], rounded once to G's type;
+ *   grad_weight[n][k] = sum over r of G[r][n] a[r][k];
+ *   grad_bias[n]      = sum over r of G[r][n].
+ *   grad_out     G [rows][outs], fp32, fp16 or bf16;
+ *   a            the product's (kept), w the weights;
+ *   grad_in      [rows][cols] of G's type, or NULL;
+ *   grad_weight  device fp32 [outs][cols], or NULL;  grad_bias fp32 [outs], or NULL;
+ *   workspace    16-byte aligned; NULL is allowed without grad_weight and grad_bias.
+ * Written arrays lie outside each other and outside what is read, and are
+ * overwritten (rows = 0: with zeros).  The products take every bit of G (as sums of
+ * bf16 values; what of it lies below 2^-126 may be lost), are summed in fp32 and in
+ * an order that depends on the sizes only.
+ * Errors: EINVAL, ESHAPE, ESPACE, EHIP. */
+int octree_nca_mx4_backward(const octnca_rows *grad_out, const octnca_mx4 *a, const octnca_mx4 *w,
+                            const octnca_rows *grad_in, float *grad_weight, float *grad_bias,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* Which elements a dropout drops.  Element e = row * cols + column (whatever the
+ * strides) draws word e & 3 of Philox4x32-10 (Salmon et al., SC 2011) with counter
+ * (e >> 2, c), each as two words, lower first, and key seed, c = index + *step
+ * (modulo 2^64); it is dropped iff the draw < T = min(2^32, floor(rate * 2^32)).
+ * Another generator than the fire mask's: its draws cost half the multiplications,
+ * and an element takes one where a cell takes one for all its channels. */
+typedef struct {
+    float rate;          /* in [0, 1] */
+    uint64_t seed;
+    uint64_t index;      /* of the mask: a layer's number, a step, .. */
+    const int64_t *step; /* device [1], read by the kernel (a captured graph draws a new mask
+                            each time it is replayed, if it counts), or NULL for 0 */
+} octnca_dropout;
+
+/* out = add + (0 if the element is dropped or not (gate > 0), else x * f), computed in
+ * fp32 and rounded once, f = 2^32 / (2^32 - T) rounded to fp32 (nothing is kept
+ * where T = 2^32).  x, gate, add, out [rows][cols] of one type; gate and add may be
+ * NULL.  With gate = x this is ReLU and dropout; with the same gate and settings
+ * and x the gradient of out, it is their gradient (rate 0: of the ReLU alone).
+ * out may be x, gate or add itself (same data and stride) and overlaps them not
+ * otherwise.  What a dropped element holds does not matter.
+ * Errors: EINVAL, ESHAPE, EHIP. */
+int octree_nca_dropout(const octnca_dropout *dropout, const octnca_rows *x, const octnca_rows *gate,
+                       const octnca_rows *add, const octnca_rows *out, int64_t rows, int64_t cols,
+                       void *stream);
+
 /* Static text for a status code; never NULL. */
 const char *octree_nca_strerror(int status);
 

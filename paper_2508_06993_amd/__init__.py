@@ -35,7 +35,10 @@ __all__ = [
     "octree_nca_state_cache_write", "octree_nca_state_cache_read", "param_structs",
     "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm",
     "octree_nca_clip_grads", "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
-    "octree_nca_train_step_kept", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
+    "octree_nca_train_step_kept", "MX4Buffers", "mx4_shapes", "octree_nca_mx4_code_bytes",
+    "octree_nca_mx4_quantise", "octree_nca_mx4_dequantise", "octree_nca_mx4_product",
+    "octree_nca_mx4_linear", "octree_nca_mx4_backward_workspace_bytes", "octree_nca_mx4_backward",
+    "octree_nca_dropout", "CODE_NAMES", "OCTNCA_BF16", "OCTNCA_CODE_I8", "OCTNCA_CODE_F8",
     "EXPORTED_SYMBOLS", "OCTNCA_OK", "OCTNCA_EINVAL",
     "OCTNCA_EUNSUPPORTED", "OCTNCA_ESHAPE",
     "OCTNCA_EHIP", "OCTNCA_ESPACE", "OCTNCA_F32", "OCTNCA_F16", "KERNEL_NAMES", "kernel_fields",
@@ -89,7 +92,9 @@ EXPORTED_SYMBOLS = (
     "octree_nca_state_cache_write", "octree_nca_state_cache_read",
     "octree_nca_param_table_bytes", "octree_nca_param_table", "octree_nca_grad_norm",
     "octree_nca_clip_grads", "octree_nca_adamw", "octree_nca_train_kept_workspace_bytes",
-    "octree_nca_train_step_kept",
+    "octree_nca_train_step_kept", "octree_nca_mx4_code_bytes", "octree_nca_mx4_quantise",
+    "octree_nca_mx4_dequantise", "octree_nca_mx4_product", "octree_nca_mx4_linear",
+    "octree_nca_mx4_backward_workspace_bytes", "octree_nca_mx4_backward", "octree_nca_dropout",
 )
 
 
@@ -146,6 +151,20 @@ class _ParamList(ctypes.Structure):
 class _AdamW(ctypes.Structure):
     _fields_ = [(k, ctypes.c_double) for k in
                 ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm", "scale", "ema_decay")]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class _MX4(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
+
+
+class _Dropout(ctypes.Structure):
+    _fields_ = [("rate", ctypes.c_float), ("seed", ctypes.c_uint64), ("index", ctypes.c_uint64),
+                ("step", ctypes.c_void_p)]
 
 
 _P = ctypes.c_void_p
@@ -220,6 +239,19 @@ _SIGS = {
     "octree_nca_clip_grads": (_I32, [ctypes.POINTER(_ParamList), ctypes.c_float, ctypes.c_float,
                                      _P, _P]),
     "octree_nca_adamw": (_I32, [ctypes.POINTER(_ParamList), ctypes.POINTER(_AdamW), _P, _P, _P]),
+    "octree_nca_mx4_code_bytes": (ctypes.c_size_t, [_I64, _I64]),
+    "octree_nca_mx4_quantise": (_I32, [ctypes.POINTER(_Rows), ctypes.POINTER(_MX4), _P]),
+    "octree_nca_mx4_dequantise": (_I32, [ctypes.POINTER(_MX4), ctypes.POINTER(_Rows), _P]),
+    "octree_nca_mx4_product": (_I32, [ctypes.POINTER(_MX4), ctypes.POINTER(_MX4), _P, _I32,
+                                      ctypes.POINTER(_Rows), _P]),
+    "octree_nca_mx4_linear": (_I32, [ctypes.POINTER(_Rows), ctypes.POINTER(_MX4),
+                                     ctypes.POINTER(_MX4), _P, _I32, ctypes.POINTER(_Rows), _P]),
+    "octree_nca_mx4_backward_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
+    "octree_nca_mx4_backward": (_I32, [ctypes.POINTER(_Rows), ctypes.POINTER(_MX4),
+                                       ctypes.POINTER(_MX4), ctypes.POINTER(_Rows), _P, _P, _P,
+                                       ctypes.c_size_t, _P]),
+    "octree_nca_dropout": (_I32, [ctypes.POINTER(_Dropout)] + [ctypes.POINTER(_Rows)] * 4 +
+                           [_I64, _I64, _P]),
     "octree_nca_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "octree_nca_abi_version": (ctypes.c_int, []),
 }
@@ -812,3 +844,151 @@ def octree_nca_adamw(plist: _ParamList, step, lr: float, betas=(0.9, 0.99), eps=
                                 _ptr(step, torch.int64, "step"),
                                 _ptr(norm, torch.float32, "norm"), _stream(stream))
     _check(st, "octree_nca_adamw")
+
+
+# ---------------------------------------------------------------------------
+# cell layers: matrices in microscaled 4 bits, dropout
+# ---------------------------------------------------------------------------
+
+def _on_device(t, name):
+    """Refuses tensors that the current device's kernels would not be given."""
+    if not t.is_cuda:
+        raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
+    if t.device.index != _current_device():
+        raise OctreeNCAError(f"{name}: on {t.device}, the current device is {_current_device()}")
+
+
+def _rows(t, name, rows=None, cols=None):
+    """octnca_rows of a tensor [..., cols]: rows any distance apart (two
+    dimensions) or contiguous; checked against a size if one is given."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    dtype = _GRAD_TYPES.get(t.dtype)
+    if dtype is None:
+        raise OctreeNCAError(f"{name}: expected fp32, fp16 or bf16, got {t.dtype}")
+    _on_device(t, name)
+    shape = t.shape
+    if len(shape) == 2:
+        r, c = shape
+        stride, step = t.stride()
+        if (step != 1 and c > 1) or (stride < c and r > 1):
+            raise OctreeNCAError(f"{name}: columns must be contiguous and rows apart, got strides "
+                                 f"{(stride, step)}")
+    else:
+        if not shape or not t.is_contiguous():
+            raise OctreeNCAError(f"{name}: expected rows of columns or a contiguous tensor")
+        c = shape[-1]
+        r = t.numel() // c if c else 0
+        stride = c
+    if rows is not None and (r, c) != (rows, cols):
+        raise OctreeNCAError(f"{name}: expected {(rows, cols)}, got {(r, c)}")
+    return _Rows(t.data_ptr(), stride, dtype), r, c
+
+
+def _vector(t, name, n):
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise OctreeNCAError(f"{name}: expected {n} elements, got {t.numel()}")
+    _on_device(t, name)
+    return _ptr(t, torch.float32, name)
+
+
+def mx4_shapes(rows: int, cols: int):
+    """Shapes of the codes and scales (uint8) of a matrix in 4 bits."""
+    groups, blocks = -(-rows // 16), -(-cols // 32)
+    return (groups, blocks, 16, 16), (groups, blocks, 16)
+
+
+@dataclass(frozen=True)
+class MX4Buffers:
+    """A matrix in microscaled 4 bits (octnca_mx4): codes and scales uint8 of
+    mx4_shapes, or of more rows."""
+    rows: int
+    cols: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def struct(self) -> _MX4:
+        for t, want, name in zip((self.codes, self.scales), mx4_shapes(self.rows, self.cols),
+                                 ("codes", "scales")):
+            shape = tuple(t.shape)
+            if shape[1:] != want[1:] or len(shape) != len(want) or shape[0] < want[0]:
+                raise OctreeNCAError(f"{name}: expected shape {want}, got {shape}")
+            _on_device(t, name)
+        return _MX4(self.rows, self.cols, _ptr(self.codes, torch.uint8, "codes"),
+                    _ptr(self.scales, torch.uint8, "scales"))
+
+
+def octree_nca_mx4_code_bytes(rows: int, cols: int) -> int:
+    return int(lib().octree_nca_mx4_code_bytes(rows, cols))
+
+
+def octree_nca_mx4_quantise(x, m: _MX4, stream=None) -> None:
+    """m (MX4Buffers.struct) = x [rows][cols] in 4 bits."""
+    st = lib().octree_nca_mx4_quantise(_rows(x, "x", m.rows, m.cols)[0], m, _stream(stream))
+    if st:
+        _check(st, "octree_nca_mx4_quantise")
+
+
+def octree_nca_mx4_dequantise(m: _MX4, x, stream=None) -> None:
+    """x [rows][cols] = the values of m."""
+    st = lib().octree_nca_mx4_dequantise(m, _rows(x, "x", m.rows, m.cols)[0], _stream(stream))
+    if st:
+        _check(st, "octree_nca_mx4_dequantise")
+
+
+def octree_nca_mx4_product(a: _MX4, w: _MX4, out, bias=None, relu=False, stream=None) -> None:
+    """out [a.rows][w.rows] = a times w transposed, plus bias; relu."""
+    st = lib().octree_nca_mx4_product(a, w, _vector(bias, "bias", w.rows), relu,
+                                      _rows(out, "out", a.rows, w.rows)[0], _stream(stream))
+    if st:
+        _check(st, "octree_nca_mx4_product")
+
+
+def octree_nca_mx4_linear(x, kept: _MX4, w: _MX4, out, bias=None, relu=False,
+                          stream=None) -> None:
+    """kept = x in 4 bits, out = kept times w transposed, plus bias; relu."""
+    st = lib().octree_nca_mx4_linear(_rows(x, "x", kept.rows, kept.cols)[0], kept, w,
+                                     _vector(bias, "bias", w.rows), relu,
+                                     _rows(out, "out", kept.rows, w.rows)[0], _stream(stream))
+    if st:
+        _check(st, "octree_nca_mx4_linear")
+
+
+def octree_nca_mx4_backward_workspace_bytes(rows: int, cols: int, outs: int) -> int:
+    return int(lib().octree_nca_mx4_backward_workspace_bytes(rows, cols, outs))
+
+
+def octree_nca_mx4_backward(grad_out, a: _MX4, w: _MX4, grad_in=None, grad_weight=None,
+                            grad_bias=None, workspace=None, stream=None) -> None:
+    """Gradients of the product of a and w for the gradient grad_out
+    [a.rows][w.rows]; grad_weight fp32 [w.rows][a.cols], grad_bias fp32 [w.rows]."""
+    if workspace is not None:
+        _on_device(workspace, "workspace")
+    st = lib().octree_nca_mx4_backward(
+        _rows(grad_out, "grad_out", a.rows, w.rows)[0], a, w,
+        None if grad_in is None else _rows(grad_in, "grad_in", a.rows, a.cols)[0],
+        _vector(grad_weight, "grad_weight", w.rows * a.cols),
+        _vector(grad_bias, "grad_bias", w.rows), _ptr(workspace, None, "workspace"),
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream(stream))
+    if st:
+        _check(st, "octree_nca_mx4_backward")
+
+
+def octree_nca_dropout(x, out, rate: float, seed: int, index=0, step=None, gate=None, add=None,
+                       stream=None) -> None:
+    """out = add + dropout of x (gated); step: device int64 [1] added to index."""
+    if step is not None:
+        if step.numel() != 1:
+            raise OctreeNCAError(f"step: expected 1 element, got {step.numel()}")
+        _on_device(step, "step")
+    rx, r, c = _rows(x, "x")
+    st = lib().octree_nca_dropout(
+        _Dropout(rate, seed, index, _ptr(step, torch.int64, "step")), rx,
+        None if gate is None else _rows(gate, "gate", r, c)[0],
+        None if add is None else _rows(add, "add", r, c)[0], _rows(out, "out", r, c)[0], r, c,
+        _stream(stream))
+    if st:
+        _check(st, "octree_nca_dropout")

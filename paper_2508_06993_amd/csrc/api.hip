@@ -1540,6 +1540,94 @@ bool list_ok(const octnca_param_list *l, int32_t need) {
 
 bool positive(double x) { return x > 0.0 && x < HUGE_VAL; }
 
+// --- cell layers -------------------------------------------------------------
+
+constexpr int64_t kMaxLayerRows = int64_t(1) << 29;
+constexpr int64_t kMaxLayerCols = int64_t(1) << 20;
+constexpr int64_t kMaxElements = int64_t(1) << 44;
+
+// A matrix of values or of codes in memory: `rows` runs of `row_bytes`, `stride`
+// bytes apart.
+struct Span {
+    const void *data;
+    size_t rows, row_bytes, stride;
+    size_t bytes() const { return rows ? (rows - 1) * stride + row_bytes : 0; }
+};
+
+Span span_of(const octnca_rows *x, int64_t rows, int64_t cols) {
+    const size_t size = dtype_bytes(x->dtype);
+    return Span{x->data, (size_t)rows, (size_t)cols * size,
+                rows > 1 ? (size_t)x->stride * size : (size_t)cols * size};
+}
+Span span_of(const void *p, size_t bytes) { return Span{p, bytes ? 1u : 0u, bytes, bytes}; }
+
+// Whether two matrices share bytes.  Of equal strides (two sets of columns of one
+// buffer) the columns decide, of others the memory from first to last byte.
+bool overlap(const Span &a, const Span &b) {
+    if (a.rows == 0 || b.rows == 0 || !overlap(a.data, a.bytes(), b.data, b.bytes())) return false;
+    if (a.rows > 1 && a.stride == b.stride) {
+        const uintptr_t pa = (uintptr_t)a.data, pb = (uintptr_t)b.data;
+        // where b's columns begin after a's, modulo the stride
+        const size_t at = pb >= pa ? (pb - pa) % a.stride
+                                   : (a.stride - (pa - pb) % a.stride) % a.stride;
+        return at < a.row_bytes || at + b.row_bytes > a.stride;
+    }
+    return true;
+}
+
+int check_rows(const octnca_rows *x, int64_t rows, int64_t cols) {
+    if (x == nullptr || !grad_type(x->dtype)) return OCTNCA_EINVAL;
+    if (rows == 0) return OCTNCA_OK;
+    if (x->data == nullptr || misaligned(x->data, dtype_bytes(x->dtype))) return OCTNCA_EINVAL;
+    if (rows > 1 && (x->stride < cols || x->stride > kMaxCacheBytes / 4 / rows)) return OCTNCA_ESHAPE;
+    return OCTNCA_OK;
+}
+
+bool mx4_size_ok(int64_t rows, int64_t cols) {
+    return rows >= 0 && rows <= kMaxLayerRows && cols >= 1 && cols <= kMaxLayerCols;
+}
+
+size_t mx4_code_bytes(int64_t rows, int64_t cols) {
+    return (size_t)((rows + 15) / 16 * mx4_blocks(cols)) * 256;
+}
+
+int check_mx4(const octnca_mx4 *m) {
+    if (m == nullptr) return OCTNCA_EINVAL;
+    if (!mx4_size_ok(m->rows, m->cols)) return OCTNCA_ESHAPE;
+    if (m->rows == 0) return OCTNCA_OK;
+    if (m->codes == nullptr || m->scales == nullptr || misaligned(m->codes, 16) ||
+        misaligned(m->scales, 16))
+        return OCTNCA_EINVAL;
+    const size_t bytes = mx4_code_bytes(m->rows, m->cols);
+    return overlap(m->codes, bytes, m->scales, bytes / 16) ? OCTNCA_EINVAL : OCTNCA_OK;
+}
+
+bool overlap(const octnca_mx4 *m, const Span &x) {
+    const size_t bytes = mx4_code_bytes(m->rows, m->cols);
+    return overlap(span_of(m->codes, bytes), x) || overlap(span_of(m->scales, bytes / 16), x);
+}
+
+bool overlap(const octnca_mx4 *a, const octnca_mx4 *b) {
+    const size_t bytes = mx4_code_bytes(b->rows, b->cols);
+    return overlap(a, span_of(b->codes, bytes)) || overlap(a, span_of(b->scales, bytes / 16));
+}
+
+// Arguments of a product of a [rows][cols] with w, its result apart.
+int check_product(const octnca_mx4 *a, const octnca_mx4 *w, const float *bias,
+                  const octnca_rows *out) {
+    int st = check_mx4(a);
+    if (st == OCTNCA_OK) st = check_mx4(w);
+    if (st) return st;
+    if (w->cols != a->cols || w->rows > kMaxLayerCols) return OCTNCA_ESHAPE;
+    if (misaligned(bias, 4)) return OCTNCA_EINVAL;
+    if (w->rows == 0) return out && grad_type(out->dtype) ? OCTNCA_OK : OCTNCA_EINVAL;
+    if ((st = check_rows(out, a->rows, w->rows))) return st;
+    const Span o = span_of(out, a->rows, w->rows);
+    if (overlap(a, o) || overlap(w, o) || (bias && overlap(span_of(bias, (size_t)w->rows * 4), o)))
+        return OCTNCA_EINVAL;
+    return OCTNCA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1628,6 +1716,131 @@ int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings
         !(h.ema_decay >= 0.0 && h.ema_decay <= 1.0))
         return OCTNCA_EINVAL;
     return hip_status(launch_adamw(*list, h, step, norm, (hipStream_t)stream));
+}
+
+size_t octree_nca_mx4_code_bytes(int64_t rows, int64_t cols) {
+    return mx4_size_ok(rows, cols) ? mx4_code_bytes(rows, cols) : 0;
+}
+
+int octree_nca_mx4_quantise(const octnca_rows *x, const octnca_mx4 *m, void *stream) {
+    int st = check_mx4(m);
+    if (st == OCTNCA_OK) st = check_rows(x, m->rows, m->cols);
+    if (st || m->rows == 0) return st;
+    if (overlap(m, span_of(x, m->rows, m->cols))) return OCTNCA_EINVAL;
+    return hip_status(launch_mx4_quantise(*x, *m, (hipStream_t)stream));
+}
+
+int octree_nca_mx4_dequantise(const octnca_mx4 *m, const octnca_rows *x, void *stream) {
+    int st = check_mx4(m);
+    if (st == OCTNCA_OK) st = check_rows(x, m->rows, m->cols);
+    if (st || m->rows == 0) return st;
+    if (overlap(m, span_of(x, m->rows, m->cols))) return OCTNCA_EINVAL;
+    return hip_status(launch_mx4_dequantise(*m, *x, (hipStream_t)stream));
+}
+
+int octree_nca_mx4_product(const octnca_mx4 *a, const octnca_mx4 *w, const float *bias,
+                           int32_t relu, const octnca_rows *out, void *stream) {
+    const int st = check_product(a, w, bias, out);
+    if (st || a->rows == 0 || w->rows == 0) return st;
+    return hip_status(launch_mx4_product(*a, *w, bias, relu != 0, *out, (hipStream_t)stream));
+}
+
+int octree_nca_mx4_linear(const octnca_rows *x, const octnca_mx4 *kept, const octnca_mx4 *w,
+                          const float *bias, int32_t relu, const octnca_rows *out, void *stream) {
+    int st = check_product(kept, w, bias, out);
+    if (st == OCTNCA_OK) st = check_rows(x, kept->rows, kept->cols);
+    if (st || kept->rows == 0) return st;
+    const Span in = span_of(x, kept->rows, kept->cols);
+    if (overlap(kept, in) || overlap(kept, w) ||
+        (bias && overlap(kept, span_of(bias, (size_t)w->rows * 4))) ||
+        (w->rows && overlap(span_of(out, kept->rows, w->rows), in)))
+        return OCTNCA_EINVAL;
+    if (w->rows == 0) return hip_status(launch_mx4_quantise(*x, *kept, (hipStream_t)stream));
+    return hip_status(launch_mx4_linear(*x, *kept, *w, bias, relu != 0, *out,
+                                        (hipStream_t)stream));
+}
+
+size_t octree_nca_mx4_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t outs) {
+    if (!mx4_size_ok(rows, cols) || outs < 1 || outs > kMaxLayerCols) return 0;
+    return mx4_backward_bytes(rows, cols, outs);
+}
+
+int octree_nca_mx4_backward(const octnca_rows *grad_out, const octnca_mx4 *a, const octnca_mx4 *w,
+                            const octnca_rows *grad_in, float *grad_weight, float *grad_bias,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+    int st = check_mx4(a);
+    if (st == OCTNCA_OK) st = check_mx4(w);
+    if (st) return st;
+    const int64_t rows = a->rows, cols = a->cols, outs = w->rows;
+    if (w->cols != cols || outs < 1 || outs > kMaxLayerCols) return OCTNCA_ESHAPE;
+    if ((st = check_rows(grad_out, rows, outs))) return st;
+    if (grad_in && (st = check_rows(grad_in, rows, cols))) return st;
+    if (grad_in && grad_in->dtype != grad_out->dtype) return OCTNCA_EINVAL;
+    if (misaligned(grad_weight, 4) || misaligned(grad_bias, 4) || misaligned(workspace, 16))
+        return OCTNCA_EINVAL;
+    const bool sums = grad_weight != nullptr || grad_bias != nullptr;
+    const size_t need = sums ? mx4_backward_bytes(rows, cols, outs) : 0;
+    if (sums && workspace == nullptr) return OCTNCA_EINVAL;
+    if (workspace_bytes < need) return OCTNCA_ESPACE;
+    // what is written, apart from each other and from what is read
+    const Span written[] = {grad_in ? span_of(grad_in, rows, cols) : Span{},
+                            span_of(grad_weight, grad_weight ? (size_t)(outs * cols) * 4 : 0),
+                            span_of(grad_bias, grad_bias ? (size_t)outs * 4 : 0),
+                            span_of(workspace, need)};
+    const Span grad = span_of(grad_out, rows, outs);
+    for (int i = 0; i < 4; ++i) {
+        if (overlap(written[i], grad) || overlap(a, written[i]) || overlap(w, written[i]))
+            return OCTNCA_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (overlap(written[i], written[j])) return OCTNCA_EINVAL;
+    }
+    return hip_status(launch_mx4_backward(*grad_out, *a, *w, grad_in, grad_weight, grad_bias,
+                                          workspace, (hipStream_t)stream));
+}
+
+int octree_nca_dropout(const octnca_dropout *dropout, const octnca_rows *x, const octnca_rows *gate,
+                       const octnca_rows *add, const octnca_rows *out, int64_t rows, int64_t cols,
+                       void *stream) {
+    uint64_t threshold;
+    if (dropout == nullptr || !fire_threshold(dropout->rate, &threshold) ||
+        misaligned(dropout->step, 8))
+        return OCTNCA_EINVAL;
+    if (rows < 0 || cols < 0) return OCTNCA_ESHAPE;
+    if (rows == 0 || cols == 0) return x && out ? OCTNCA_OK : OCTNCA_EINVAL;
+    if (rows > kMaxElements / cols) return OCTNCA_ESHAPE;
+    const octnca_rows *all[] = {x, gate, add, out};
+    for (int i = 0; i < 4; ++i) {
+        if (all[i] == nullptr && (i == 1 || i == 2)) continue;
+        const int st = check_rows(all[i], rows, cols);
+        if (st) return st;
+        if (all[i]->dtype != x->dtype) return OCTNCA_EINVAL;
+    }
+    const Span o = span_of(out, rows, cols);
+    for (int i = 0; i < 3; ++i) {
+        if (all[i] == nullptr) continue;
+        const Span s = span_of(all[i], rows, cols);
+        if (overlap(o, s) && !(s.data == o.data && s.stride == o.stride)) return OCTNCA_EINVAL;
+    }
+    if (dropout->step && overlap(o, span_of(dropout->step, 8))) return OCTNCA_EINVAL;
+    DropArgs d{};
+    d.x = x->data;
+    d.gate = gate ? gate->data : nullptr;
+    d.add = add ? add->data : nullptr;
+    d.out = out->data;
+    // one row has any stride
+    const auto stride = [&](const octnca_rows *r) { return r == nullptr || rows == 1 ? cols : r->stride; };
+    d.x_stride = stride(x);
+    d.gate_stride = stride(gate);
+    d.add_stride = stride(add);
+    d.out_stride = stride(out);
+    d.rows = rows;
+    d.cols = cols;
+    d.seed = dropout->seed;
+    d.index = dropout->index;
+    d.step = dropout->step;
+    d.threshold = (uint32_t)threshold;   // 2^32: nothing is kept, by the factor
+    d.factor = threshold >> 32 ? 0.0f : (float)(4294967296.0 / (4294967296.0 - (double)threshold));
+    return hip_status(launch_dropout(x->dtype, d, (hipStream_t)stream));
 }
 
 }  // extern "C"

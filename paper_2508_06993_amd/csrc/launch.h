@@ -239,6 +239,33 @@ hipError_t launch_clip_grads(const octnca_param_list &l, double scale, double ma
 hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64_t *step,
                         float *norm, hipStream_t stream);
 
+// Cell layers (mx4.hip, mx4_backward.hip, dropout.hip).  Sizes are checked;
+// rows > 0.
+inline int64_t mx4_blocks(int64_t cols) { return (cols + 31) / 32; }
+hipError_t launch_mx4_quantise(const octnca_rows &x, const octnca_mx4 &m, hipStream_t stream);
+hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipStream_t stream);
+hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const float *bias,
+                              bool relu, const octnca_rows &out, hipStream_t stream);
+hipError_t launch_mx4_linear(const octnca_rows &x, const octnca_mx4 &kept, const octnca_mx4 &w,
+                             const float *bias, bool relu, const octnca_rows &out,
+                             hipStream_t stream);
+size_t mx4_backward_bytes(int64_t rows, int64_t cols, int64_t outs);
+// grad_in, grad_weight, grad_bias may be null; rows may be 0.
+hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
+                               const octnca_mx4 &w, const octnca_rows *grad_in, float *grad_weight,
+                               float *grad_bias, void *workspace, hipStream_t stream);
+struct DropArgs {
+    const void *x, *gate, *add;   // gate, add may be null
+    void *out;
+    int64_t x_stride, gate_stride, add_stride, out_stride;
+    int64_t rows, cols;
+    uint64_t seed, index;
+    const int64_t *step;          // or null
+    uint32_t threshold;           // draws below are dropped
+    float factor;                 // of what is kept; 0: nothing is
+};
+hipError_t launch_dropout(int32_t dtype, const DropArgs &a, hipStream_t stream);
+
 // Compute units of the current device, cached per device.  Host threads may
 // call this concurrently: racing first calls store the same value.
 inline int device_cus() {

@@ -1,0 +1,102 @@
+// Device-side building blocks of matrices in microscaled 4 bits (octnca_mx4).
+// Internal header (not part of the ABI).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "values.h"
+
+namespace octnca {
+
+constexpr int kMxBlock = 32;      // columns that share a scale
+constexpr int kMxGroup = 16;      // rows whose blocks lie together: 256 bytes of codes a block
+constexpr uint32_t kMxNan = 255;  // scale byte of a block of NaN
+
+typedef float v4f32 __attribute__((ext_vector_type(4)));
+typedef int v8i32 __attribute__((ext_vector_type(8)));
+
+// Scale byte of a block from the largest magnitude's bits.  a = m 2^e with
+// 1 <= m < 2: a <= 6 * 2^k = 1.5 * 2^(k + 2) from k = e - 2 on if m <= 1.5, else
+// from e - 1; the addition carries into the exponent in the second case.  What is
+// not finite has bits of at least 0x7f800000, above those of all numbers.
+__device__ __forceinline__ uint32_t mx4_scale(uint32_t top) {
+    const int byte = (int)((top + 0x3fffffu) >> 23) - 2;
+    return top >= 0x7f800000u ? kMxNan : (uint32_t)(byte > 0 ? byte : 0);
+}
+
+// Power of two that takes a block's values to its codes' (0 for a block of NaN).
+__device__ __forceinline__ float mx4_inverse(uint32_t scale) {
+    return __uint_as_float(scale == kMxNan ? 0u : (254u - scale) << 23);
+}
+
+// Value of a scale byte: 2^-127 is a subnormal number.
+__device__ __forceinline__ float mx4_scale_value(uint32_t scale) {
+    return __uint_as_float(scale == 0 ? 0x00400000u : scale == kMxNan ? 0x7fc00000u : scale << 23);
+}
+
+// Codes of eight values times `inverse` (exact: a power of two), the first
+// lowest.  A block of NaN has codes 0.
+__device__ __forceinline__ uint32_t mx4_codes(const float *x, float inverse) {
+    if (inverse == 0.0f) return 0;
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * inverse, x[1] * inverse, 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * inverse, x[3] * inverse, 1.0f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inverse, x[5] * inverse, 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inverse, x[7] * inverse, 1.0f, 3);
+}
+
+// The values of eight codes (without their scale).
+__device__ __forceinline__ void mx4_values(uint32_t c, float *x) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const auto v = k == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0)
+                       : k == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1)
+                       : k == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2)
+                                : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
+        x[2 * k] = v[0];
+        x[2 * k + 1] = v[1];
+    }
+}
+
+// A matrix as the kernels see it.
+struct Mx4View {
+    uint8_t *codes, *scales;
+    int64_t rows;
+    int blocks;   // of a row
+};
+inline Mx4View mx4_view(const octnca_mx4 &m) {
+    return Mx4View{(uint8_t *)m.codes, (uint8_t *)m.scales, m.rows,
+                   (int)((m.cols + kMxBlock - 1) / kMxBlock)};
+}
+
+// A lane's part of 16 rows times four blocks (128 columns): row lane % 16 of the
+// group, block lane / 16 of the four, as the matrix instruction wants it.  The
+// four blocks of a group are 1 KB in a row.
+struct Mx4Operand {
+    Words4 codes;
+    uint32_t scale;
+};
+
+// Blocks past the last have codes 0 and scale 1.
+__device__ __forceinline__ Mx4Operand mx4_operand(const Mx4View &m, int64_t group, int block) {
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (group * m.blocks + block) * kMxGroup + lane;
+    Mx4Operand o{Words4{0, 0, 0, 0}, 127};
+    if (block + lane / kMxGroup < m.blocks) {
+        o.codes = ((const Words4 *)m.codes)[at];
+        o.scale = m.scales[at];
+    }
+    return o;
+}
+
+// acc[i] of lane l += sum over 128 columns of a's row 4 (l / 16) + i times b's row
+// l % 16.
+__device__ __forceinline__ v4f32 mx4_mfma(const Mx4Operand &a, const Mx4Operand &b, v4f32 acc) {
+    const v8i32 x = {(int)a.codes[0], (int)a.codes[1], (int)a.codes[2], (int)a.codes[3], 0, 0, 0, 0};
+    const v8i32 y = {(int)b.codes[0], (int)b.codes[1], (int)b.codes[2], (int)b.codes[3], 0, 0, 0, 0};
+    // 4, 4: both operands e2m1; byte 0 of each lane's scale
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, a.scale, 0, b.scale);
+}
+
+}  // namespace octnca

@@ -1,6 +1,6 @@
 """Convenience layer over the binding: upload weights, allocate the workspace
-and outputs with PyTorch, run ``octree_nca_infer``; state caches, parameter lists
-and training.  Allocation and marshalling only; the computation is the library's.
+and outputs with PyTorch, run ``octree_nca_infer``; state caches, parameter lists,
+training and cell layers.  Allocation and marshalling only; the computation is the library's.
 """
 from __future__ import annotations
 
@@ -11,12 +11,15 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (Model, OctreeNCAError, StateCacheBuffers, _stream, _cache_call, check_train_weights,
-               lib, octree_nca_adamw, octree_nca_clip_grads, octree_nca_grad_norm, octree_nca_infer,
+from . import (Model, MX4Buffers, OctreeNCAError, StateCacheBuffers, _stream, _cache_call, check_train_weights,
+               lib, octree_nca_adamw, octree_nca_clip_grads, octree_nca_dropout, octree_nca_grad_norm,
+               octree_nca_infer, octree_nca_mx4_backward,
+               octree_nca_mx4_backward_workspace_bytes, octree_nca_mx4_dequantise,
+               octree_nca_mx4_linear, octree_nca_mx4_product, octree_nca_mx4_quantise,
                octree_nca_param_table, octree_nca_param_table_bytes,
                octree_nca_train_kept_workspace_bytes, octree_nca_train_step,
                octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
-               octree_nca_workspace_bytes, param_structs, state_cache_refs)
+               octree_nca_workspace_bytes, param_structs, state_cache_refs, mx4_shapes)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
 
@@ -277,3 +280,128 @@ class Trainer:
         loss = self.gradients(image, target, fire_rate, seed, stream=stream)
         norm = self.parameters.adamw(stream=stream, **{**self.settings, **settings})
         return loss, norm
+
+
+class MX4Matrix:
+    """Rows of values in microscaled 4 bits (octnca_mx4), 17 bytes for 32 columns:
+    ``rows`` of them at most, ``used`` by the last quantise.  ``codes`` /
+    ``scales``: device memory of mx4_shapes to use instead of new."""
+
+    def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None, device="cuda"):
+        self.rows, self.cols = int(rows), int(cols)
+        shapes = mx4_shapes(self.rows, self.cols)
+        own = []
+        if codes is None:
+            codes = torch.zeros(shapes[0], dtype=torch.uint8, device=device)
+            own.append(codes)
+        if scales is None:
+            scales = torch.zeros(shapes[1], dtype=torch.uint8, device=device)
+            own.append(scales)
+        self.buffers = MX4Buffers(self.rows, self.cols, codes, scales)
+        self.struct = self.buffers.struct()
+        self._own = _Buffers(*own)
+
+    @property
+    def used(self) -> int:
+        return self.struct.rows
+
+    @used.setter
+    def used(self, n: int):
+        if not 0 <= n <= self.rows:
+            raise OctreeNCAError(f"{n} rows, the matrix has room for {self.rows}")
+        self.struct.rows = n
+
+    def quantise(self, x: torch.Tensor, stream=None) -> "MX4Matrix":
+        """Takes x [...][cols], of fp32, fp16 or bf16."""
+        self.used = x.numel() // self.cols
+        octree_nca_mx4_quantise(x, self.struct, self._own.use(stream))
+        return self
+
+    def dequantise(self, out: torch.Tensor, stream=None) -> torch.Tensor:
+        """Fills and returns ``out`` [...][cols] with the rows in use."""
+        octree_nca_mx4_dequantise(self.struct, out, self._own.use(stream))
+        return out
+
+
+class CellLayer:
+    """A linear layer on every cell, out = x weight^T + bias, with weights and
+    inputs in microscaled 4 bits.
+
+    ``weight`` [outs][cols] and ``bias`` (fp32 [outs] or None) stay the caller's;
+    ``refresh`` takes the weights over after they change.  ``rows``: the most cells
+    of a call.  ``train``: with memory for the gradients ``grad_weight`` and
+    ``grad_bias`` (fp32).  Calls of one layer must not overlap: it holds the kept
+    inputs and the gradients.  Calls on any stream come after what the constructor
+    enqueued, and are ordered among each other by the caller."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, rows=1,
+                 train=False):
+        if weight.dim() != 2:
+            raise OctreeNCAError(f"weight: expected [outs][cols], got {tuple(weight.shape)}")
+        self.weight, self.bias = weight, bias
+        self.outs, self.cols = weight.shape
+        self.w = MX4Matrix(self.outs, self.cols, device=weight.device)
+        self.kept = MX4Matrix(rows, self.cols, device=weight.device)
+        self.grad_weight = self.grad_bias = self.workspace = None
+        own = [self.w.buffers.codes, self.w.buffers.scales, self.kept.buffers.codes,
+               self.kept.buffers.scales]
+        if train:
+            size = octree_nca_mx4_backward_workspace_bytes(rows, self.cols, self.outs)
+            if size == 0:
+                raise OctreeNCAError("CellLayer: invalid rows or weights")
+            device = weight.device
+            self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
+            self.grad_weight = torch.zeros((self.outs, self.cols), device=device)
+            self.grad_bias = torch.zeros(self.outs, device=device) if bias is not None else None
+            own += [t for t in (self.workspace, self.grad_weight, self.grad_bias) if t is not None]
+        self.refresh()
+        self._own = _Buffers(*own)
+
+    def refresh(self, stream=None) -> None:
+        """Takes ``weight`` over."""
+        self.w.quantise(self.weight, stream)
+
+    def forward(self, x, out: torch.Tensor, relu=False, stream=None) -> torch.Tensor:
+        """Fills and returns ``out`` [...][outs].  x: [...][cols], left in 4 bits in
+        ``kept``; or an MX4Matrix of such rows."""
+        stream = self._own.use(stream)
+        if isinstance(x, MX4Matrix):
+            octree_nca_mx4_product(x.struct, self.w.struct, out, self.bias, relu,
+                                   x._own.use(stream))
+        else:
+            self.kept.used = x.numel() // self.cols
+            octree_nca_mx4_linear(x, self.kept.struct, self.w.struct, out, self.bias, relu, stream)
+        return out
+
+    def backward(self, grad_out: torch.Tensor, grad_in: Optional[torch.Tensor] = None,
+                 kept: Optional[MX4Matrix] = None, stream=None) -> None:
+        """Fills ``grad_weight`` and ``grad_bias``, and grad_in [...][cols] (of
+        grad_out's type) if given, for the gradient of the last forward's out
+        (without its relu), or of that of the rows ``kept``."""
+        if self.workspace is None:
+            raise OctreeNCAError("CellLayer: made without train=True")
+        stream = self._own.use(stream)
+        if kept is not None:
+            kept._own.use(stream)
+        octree_nca_mx4_backward(grad_out, (kept or self.kept).struct, self.w.struct, grad_in,
+                                self.grad_weight, self.grad_bias, self.workspace, stream)
+
+
+class Dropout:
+    """Dropout with a mask that is drawn anew in every call (octnca_dropout).
+
+    ``step``: device int64 [1] that counts training steps, read by the kernel and
+    added to ``index``, so that a captured graph draws a new mask each time it is
+    replayed; the gradient has to see the same value as the forward."""
+
+    def __init__(self, rate: float, seed: int, step: Optional[torch.Tensor] = None):
+        self.rate, self.seed, self.step = float(rate), int(seed), step
+
+    def __call__(self, x: torch.Tensor, out: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                 add: Optional[torch.Tensor] = None, index=0, stream=None) -> torch.Tensor:
+        """Fills and returns ``out`` (which may be x, gate or add): x where it is
+        kept and gate > 0, scaled, plus ``add``.  ReLU and dropout: gate = x; their
+        gradient: x the gradient, the same gate and index."""
+        octree_nca_dropout(x, out, self.rate, self.seed, index, self.step, gate, add, stream)
+        return out
