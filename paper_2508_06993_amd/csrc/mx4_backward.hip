@@ -5,6 +5,7 @@
 // split into bf16 parts that add up to it: bf16 one, fp16 two, fp32 three.  So every
 // product is exact and only the fp32 sums round.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 #include "mx4.h"
@@ -14,11 +15,12 @@ namespace octnca {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 64;      // rows and columns of a workgroup's tile of the result
-constexpr int kStep = 32;      // of the summed index
-constexpr int kPitch = 40;     // of a tile's rows in LDS, bf16 values
+constexpr int kStep = 32;      // of the summed index: the matrix instruction's
+constexpr int kPad = 16;       // values after a row of a tile in LDS: four rows of 32 bytes are
+                               // read at once, from different banks
 
 typedef __bf16 v8bf16 __attribute__((ext_vector_type(8)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
 
 template <typename V> constexpr int kParts = 3;
 template <> constexpr int kParts<Values<OCTNCA_F16>> = 2;
@@ -46,147 +48,523 @@ struct BackwardArgs {
     int64_t stride;
     int64_t rows;
     int outs, cols;
+    bool vec;             // G's rows start at multiples of 16 bytes and have 8 n values
     Mx4View q;            // the weights (grad_in) or the inputs (grad_weight)
-    void *out;            // grad_in
+    void *out;            // grad_in, or grad_weight's sums [splits][outs][cols] or null
     int64_t out_stride;
-    float *sums;          // grad_weight: [splits][outs][cols], then bias [splits][outs]
-    float *bias;          // or null
+    bool out_vec;         // out's rows start at multiples of four values
+    float *bias;          // sums [splits][outs], or null
     int64_t per_split;    // rows of a split (a multiple of kStep)
 };
 
+// A tile of bf16 values in LDS, the summed index along the rows: the operand of 16
+// columns from `col` on.  Lane l gets column l % 16, eight rows from 8 (l / 16) on:
+// each read hands four rows of sixteen columns out to sixteen lanes, transposed.
+template <int PITCH>
+__device__ __forceinline__ v8bf16 read_columns(const uint16_t *tile, int col) {
+    typedef __attribute__((address_space(3))) v4i16 *Lds;
+    const int lane = threadIdx.x & 63;
+    const uint16_t *at = tile + (lane / 16 * 8 + lane % 16 / 4) * PITCH + col + lane % 4 * 4;
+    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+    const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * PITCH));
+    return __builtin_bit_cast(v8bf16, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Eight values of G as loaded, ahead of their use.
+template <typename V> struct Raw8 {
+    Words4 w[V::kBytes / 2];
+    // Columns col .. col + 7 of a row of `end` (zeros past it, and everywhere where
+    // `in` is false; the row can be read all the same).  No branches: what lies
+    // outside is read from the row's last columns and replaced.  VEC: rows are
+    // aligned, of a multiple of eight columns.
+    template <bool VEC>
+    __device__ __forceinline__ void load(const typename V::T *row, int64_t col, int64_t end,
+                                         bool in) {
+        if (VEC) {
+            const bool all = in && col < end;
+            const Words4 *from = (const Words4 *)(row + (col < end ? col : 0));
+            const uint32_t mask = all ? ~0u : 0u;
+#pragma unroll
+            for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k] & mask;
+        } else {
+            typename V::T x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                x[k] = row[col + k < end ? col + k : end - 1];
+                if (!in || col + k >= end) x[k] = (typename V::T)0.0f;
+            }
+            __builtin_memcpy(w, x, sizeof(w));
+        }
+    }
+    __device__ __forceinline__ void values(float *x) const {
+        typename V::T v[8];
+        __builtin_memcpy(v, w, sizeof(w));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = (float)v[k];
+    }
+    // part p of the eight, packed
+    template <int P> __device__ __forceinline__ void parts(Words4 *out) const {
+        if (P == 1) {   // bf16 as it is
+            out[0] = w[0];
+            return;
+        }
+        float x[8];
+        values(x);
+        uint16_t part[8][P];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) split<P>(x[k], part[k]);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                out[p][k] = part[2 * k][p] | (uint32_t)part[2 * k + 1][p] << 16;
+    }
+};
+
+// Eight codes as bf16 values (exact).
+__device__ __forceinline__ Words4 code_values(uint32_t codes, uint32_t scale) {
+    const float s = mx4_scale_value(scale);
+    Words4 out;
+    float v[8];
+    mx4_values(codes, v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        out[k] = __float_as_uint(v[2 * k] * s) >> 16 |
+                 (__float_as_uint(v[2 * k + 1] * s) & 0xffff0000u);
+    return out;
+}
+
 // out[i][j] = sum over c of P[i][c] Q[c][j], Q the values of a matrix in 4 bits.
 // WEIGHT: i an output, c a row of G, j a column of the inputs (P = G^T); else i a
-// row of G, c an output, j a column of the weights.
-template <typename V, bool WEIGHT>
+// row of G, c an output, j a column of the weights.  A workgroup takes 32 I rows and
+// 32 J columns, four waves with a quarter each.  The next step's values are on
+// their way into registers while this one's are multiplied.
+template <typename V, bool WEIGHT, int I, int J, bool VEC>
 __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     constexpr int kP = kParts<V>;
-    __shared__ __align__(16) uint16_t ps[kP][kTile][kPitch];
-    __shared__ __align__(16) uint16_t qs[kTile][kPitch];
+    constexpr int kBi = 32 * I, kBj = 32 * J;
+    constexpr int kPitchP = WEIGHT ? kBi + kPad : kStep + 8;
+    constexpr int kRowsP = WEIGHT ? kStep : kBi;
+    constexpr int kPitchQ = kBj + kPad;
+    constexpr int kLoadsP = kBi / 64, kLoadsQ = kBj / 64;
+    static_assert(kBi % 64 == 0 && kBj % 64 == 0, "whole loads");
+    __shared__ __align__(16) uint16_t ps[2][kP][kRowsP * kPitchP];
+    __shared__ __align__(16) uint16_t qs[2][kStep * kPitchQ];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i0 = WEIGHT ? (int64_t)blockIdx.y * kTile : (int64_t)blockIdx.x * kTile;
-    const int j0 = WEIGHT ? blockIdx.x * kTile : blockIdx.y * kTile;
+    const int64_t i0 = (WEIGHT ? (int64_t)blockIdx.y : (int64_t)blockIdx.x) * kBi;
+    const int j0 = (WEIGHT ? blockIdx.x : blockIdx.y) * kBj;
     const int64_t i_end = WEIGHT ? b.outs : b.rows;
     const int64_t c_begin = WEIGHT ? (int64_t)blockIdx.z * b.per_split : 0;
     const int64_t c_end = WEIGHT ? std::min(b.rows, c_begin + b.per_split) : b.outs;
     const bool sum_bias = WEIGHT && b.bias != nullptr && j0 == 0;
     const auto grad = (const typename V::T *)b.grad;
-    v4f32 acc[2][2] = {};
-    float bias = 0.0f;
-    for (int64_t c0 = c_begin; c0 < c_end; c0 += kStep) {
-        if (WEIGHT) {
-            // a thread takes a column of G, eight rows of it
-            const int64_t i = i0 + lane;
-            uint16_t part[8][kP];
+
+    Raw8<V> p[kLoadsP];
+    uint32_t codes[kLoadsQ], scales[kLoadsQ];
+    // where a thread's part k of P lies: row and first column of the tile
+    const auto p_row = [&](int k) {
+        return WEIGHT ? (threadIdx.x + k * kThreads) / (kBi / 8) : threadIdx.x / 4 + k * 64;
+    };
+    const auto p_col = [&](int k) {
+        return WEIGHT ? (threadIdx.x + k * kThreads) % (kBi / 8) * 8 : threadIdx.x % 4 * 8;
+    };
+    const auto load = [&](int64_t c0) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int64_t c = c0 + wave * 8 + k;
-                const float x = i < i_end && c < c_end ? V::get(grad + c * b.stride + i) : 0.0f;
-                bias += x;
-                split<kP>(x, part[k]);
-            }
+        for (int k = 0; k < kLoadsP; ++k) {
+            const int64_t row = (WEIGHT ? c0 : i0) + p_row(k), rows = WEIGHT ? c_end : i_end;
+            p[k].template load<VEC>(grad + std::min(row, rows - 1) * b.stride,
+                                    (WEIGHT ? i0 : c0) + p_col(k), WEIGHT ? i_end : c_end,
+                                    row < rows);
+        }
+        // a wave takes a block of a row group: 256 bytes
 #pragma unroll
-            for (int p = 0; p < kP; ++p)
+        for (int k = 0; k < kLoadsQ; ++k) {
+            const int unit = k * 4 + wave, block = j0 / kMxBlock + unit / 2;
+            const int64_t c = c0 + unit % 2 * kMxGroup + lane / 4;
+            const bool in = c < c_end && block < b.q.blocks;
+            const int64_t row = std::min(c, c_end - 1);
+            const int64_t at = (row / kMxGroup * b.q.blocks + std::min(block, b.q.blocks - 1)) *
+                                   kMxGroup + row % kMxGroup;
+            codes[k] = ((const uint32_t *)b.q.codes)[at * 4 + lane % 4];
+            scales[k] = b.q.scales[at];
+            if (!in) codes[k] = 0, scales[k] = 127;
+        }
+    };
+    float bias[8] = {};
+    const auto store = [&](int buffer) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) ps[p][lane][wave * 8 + k] = part[k][p];
-        } else {
-            const int64_t i = i0 + threadIdx.x / 4;
+        for (int k = 0; k < kLoadsP; ++k) {
+            Words4 part[kP];
+            p[k].template parts<kP>(part);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int64_t c = c0 + threadIdx.x % 4 * 8 + k;
-                const float x = i < i_end && c < c_end ? V::get(grad + i * b.stride + c) : 0.0f;
-                uint16_t part[kP];
-                split<kP>(x, part);
+            for (int q = 0; q < kP; ++q)
+                *(Words4 *)&ps[buffer][q][p_row(k) * kPitchP + p_col(k)] = part[q];
+            if (sum_bias) {   // a thread's parts are of the same eight columns
+                float x[8];
+                p[k].values(x);
 #pragma unroll
-                for (int p = 0; p < kP; ++p)
-                    ps[p][threadIdx.x / 4][threadIdx.x % 4 * 8 + k] = part[p];
+                for (int e = 0; e < 8; ++e) bias[e] += x[e];
             }
         }
-        {
-            // a thread takes eight columns of a row of Q
-            const int64_t c = c0 + threadIdx.x / 8;
-            const int j = j0 + threadIdx.x % 8 * 8, block = j / kMxBlock;
-            float v[8] = {};
-            if (c < c_end && block < b.q.blocks) {
-                const int64_t at = (c / kMxGroup * b.q.blocks + block) * kMxGroup + c % kMxGroup;
-                mx4_values(((const uint32_t *)b.q.codes)[at * 4 + j % kMxBlock / 8], v);
-                const float scale = mx4_scale_value(b.q.scales[at]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= scale;
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                qs[threadIdx.x % 8 * 8 + k][threadIdx.x / 8] =
-                    (uint16_t)(__float_as_uint(v[k]) >> 16);
+        for (int k = 0; k < kLoadsQ; ++k) {
+            const int unit = k * 4 + wave;
+            *(Words4 *)&qs[buffer][(unit % 2 * kMxGroup + lane / 4) * kPitchQ +
+                                   unit / 2 * kMxBlock + lane % 4 * 8] =
+                code_values(codes[k], scales[k]);
         }
+    };
+
+    v4f32 acc[I][J] = {};
+    const int wi = wave % 2 * (16 * I), wj = wave / 2 * (16 * J);
+    if (c_begin < c_end) {
+        load(c_begin);
+        store(0);
+    }
+    int buffer = 0;
+    for (int64_t c0 = c_begin; c0 < c_end; c0 += kStep, buffer ^= 1) {
         __syncthreads();
-        v8bf16 q[2];
+        load(c0 + kStep);   // past the end: zeros, used by no one
+        v8bf16 q[J];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-            q[t] = *(const v8bf16 *)&qs[wave / 2 * 32 + t * 16 + lane % 16][lane / 16 * 8];
+        for (int t = 0; t < J; ++t) q[t] = read_columns<kPitchQ>(qs[buffer], wj + t * 16);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < I; ++s)
 #pragma unroll
-            for (int p = kP - 1; p >= 0; --p) {
+            for (int k = kP - 1; k >= 0; --k) {
                 const v8bf16 g =
-                    *(const v8bf16 *)&ps[p][wave % 2 * 32 + s * 16 + lane % 16][lane / 16 * 8];
+                    WEIGHT ? read_columns<kPitchP>(ps[buffer][k], wi + s * 16)
+                           : *(const v8bf16 *)&ps[buffer][k][(wi + s * 16 + lane % 16) * kPitchP +
+                                                             lane / 16 * 8];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < J; ++t)
                     acc[s][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t], g, acc[s][t], 0, 0, 0);
             }
-        __syncthreads();
+        store(buffer ^ 1);
     }
     // a lane has four columns j of row i
+    using O = std::conditional_t<WEIGHT, Values<OCTNCA_F32>, V>;
+    auto out = (typename O::T *)b.out;
+    if (WEIGHT && out) out += (int64_t)blockIdx.z * b.outs * b.cols;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < I; ++s)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int64_t i = i0 + wave % 2 * 32 + s * 16 + lane % 16;
-            const int j = j0 + wave / 2 * 32 + t * 16 + lane / 16 * 4;
-            if (i >= i_end) continue;
+        for (int t = 0; t < J; ++t) {
+            const int64_t i = i0 + wi + s * 16 + lane % 16;
+            const int j = j0 + wj + t * 16 + lane / 16 * 4;
+            if (i >= i_end || (WEIGHT && out == nullptr)) continue;
+            const float y[4] = {acc[s][t][0], acc[s][t][1], acc[s][t][2], acc[s][t][3]};
+            auto to = out + i * b.out_stride + j;
+            if (b.out_vec && j + 4 <= b.cols) {
+                O::put4(to, y);
+            } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (j + k >= b.cols) continue;
-                if (WEIGHT)
-                    b.sums[((int64_t)blockIdx.z * b.outs + i) * b.cols + j + k] = acc[s][t][k];
-                else
-                    V::put((typename V::T *)b.out + i * b.out_stride + j + k, acc[s][t][k]);
+                for (int k = 0; k < 4; ++k)
+                    if (j + k < b.cols) O::put(to + k, y[k]);
             }
         }
     if (sum_bias) {
-        float *sums = (float *)ps;   // every wave has passed the last barrier
-        sums[threadIdx.x] = bias;
+        // kBi / 8 threads hold the columns, the others more rows of them
+        constexpr int kSets = kThreads / (kBi / 8);
+        __shared__ float sums[kSets][kBi];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sums[threadIdx.x / (kBi / 8)][threadIdx.x % (kBi / 8) * 8 + e] = bias[e];
         __syncthreads();
-        if (wave == 0 && i0 + lane < i_end)
-            b.bias[(int64_t)blockIdx.z * b.outs + i0 + lane] =
-                (sums[lane] + sums[lane + 64]) + (sums[lane + 128] + sums[lane + 192]);
+        for (int i = threadIdx.x; i < kBi; i += kThreads) {
+            float x = 0.0f;
+            for (int k = 0; k < kSets; ++k) x += sums[k][i];
+            if (i0 + i < i_end) b.bias[(int64_t)blockIdx.z * b.outs + i0 + i] = x;
+        }
     }
 }
 
-// to[e] = sum over the splits, in order
-__global__ __launch_bounds__(kThreads) void join(const float *__restrict__ sums, float *to,
-                                                 int64_t n, int splits) {
-    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < n;
-         e += (int64_t)gridDim.x * kThreads) {
-        double x = 0.0;
-        for (int s = 0; s < splits; ++s) x += sums[s * n + e];
-        to[e] = (float)x;
+// Narrow layers: at most 32 NT outputs and 16 KT columns, any number of rows.  One
+// pass over G gives all three gradients.  A wave takes 32 rows at a time: G goes from
+// memory straight into the operands of grad_in, whose other operand (the weights)
+// stays in registers, and through the wave's part of LDS, transposed, into those of
+// grad_weight, whose sums stay in registers over all of the wave's rows.
+struct NarrowArgs {
+    const void *grad;
+    int64_t stride;
+    int rows, outs, cols;
+    Mx4View a, w;
+    void *in;             // grad_in or null
+    int64_t in_stride;
+    bool in_vec;
+    float *sums;          // [splits][outs][cols] or null
+    float *bias;          // [splits][outs] or null
+};
+
+// Orders a wave's own LDS accesses.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <typename V, int NT, int KT, bool VEC>
+__global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
+    constexpr int kP = kParts<V>, kWaves = kThreads / 64;
+    constexpr int kN = 32 * NT, kK = 16 * KT, kB = KT / 2;   // kB: blocks of a row
+    constexpr int kPitchG = kN + kPad, kPitchA = kK + kPad;
+    constexpr int kWaveBytes = 2 * kStep * (kP * kPitchG + kPitchA);
+    constexpr int kSumBytes = 4 * kN * (kK + 1);
+    constexpr int kW = 2 * kN * kPitchA;
+    constexpr int kLds = std::max(kWaves * std::max(kWaveBytes, kSumBytes), kW);
+    __shared__ __align__(16) char lds[kLds];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    // the weights as operands
+    v8bf16 w[NT][KT];
+    {
+        uint16_t *t = (uint16_t *)lds;
+        for (int u = wave; u < 2 * NT * kB; u += kWaves) {   // a block of a row group each
+            const int group = u / kB, block = u % kB, n = group * kMxGroup + lane / 4;
+            uint32_t codes = 0, scale = 127;
+            if (n < b.outs && block < b.w.blocks) {
+                const int at = (group * b.w.blocks + block) * kMxGroup + lane / 4;
+                codes = ((const uint32_t *)b.w.codes)[at * 4 + lane % 4];
+                scale = b.w.scales[at];
+            }
+            *(Words4 *)&t[n * kPitchA + block * kMxBlock + lane % 4 * 8] = code_values(codes, scale);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) w[n][k] = read_columns<kPitchA>(t + n * 32 * kPitchA, k * 16);
+        __syncthreads();
     }
+    uint16_t *gs = (uint16_t *)(lds + wave * kWaveBytes);   // [kP][kStep][kPitchG]
+    uint16_t *as = gs + kP * kStep * kPitchG;               // [kStep][kPitchA]
+
+    Raw8<V> raw[2][NT];
+    uint32_t codes[2][kB], scales[2][kB];
+    const auto load = [&](int step) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int row = step * kStep + g * kMxGroup + lane % kMxGroup;
+            const auto from = (const typename V::T *)b.grad + (int64_t)std::min(row, b.rows - 1) * b.stride;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                raw[g][n].template load<VEC>(from, n * 32 + lane / 16 * 8, b.outs, row < b.rows);
+            const int arow = step * kStep + g * kMxGroup + lane / 4;
+#pragma unroll
+            for (int k = 0; k < kB; ++k) {
+                const int r = std::min(arow, b.rows - 1);
+                const int64_t at = ((int64_t)(r / kMxGroup) * b.a.blocks + std::min(k, b.a.blocks - 1)) *
+                                       kMxGroup + r % kMxGroup;
+                codes[g][k] = ((const uint32_t *)b.a.codes)[at * 4 + lane % 4];
+                scales[g][k] = b.a.scales[at];
+                if (arow >= b.rows || k >= b.a.blocks) codes[g][k] = 0, scales[g][k] = 127;
+            }
+        }
+    };
+    const __bf16 one = (__bf16)1.0f;
+    const v8bf16 ones = {one, one, one, one, one, one, one, one};
+    v4f32 acc[2 * NT][KT] = {}, acc_bias[2 * NT] = {};
+    const int steps = (b.rows + kStep - 1) / kStep, all = gridDim.x * kWaves;
+    int step = blockIdx.x * kWaves + wave;
+    if (step < steps) load(step);
+    for (; step < steps; step += all) {
+        // this step's operands, in registers and LDS
+        Words4 part[2][NT][kP];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                raw[g][n].template parts<kP>(part[g][n]);
+#pragma unroll
+                for (int p = 0; p < kP; ++p)
+                    *(Words4 *)&gs[(p * kStep + g * kMxGroup + lane % 16) * kPitchG + n * 32 +
+                                   lane / 16 * 8] = part[g][n][p];
+            }
+#pragma unroll
+            for (int k = 0; k < kB; ++k)
+                *(Words4 *)&as[(g * kMxGroup + lane / 4) * kPitchA + k * kMxBlock + lane % 4 * 8] =
+                    code_values(codes[g][k], scales[g][k]);
+        }
+        load(step + all);   // past the end: zeros, used by no one
+        if (b.in) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int row = step * kStep + g * kMxGroup + lane % kMxGroup;
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    v4f32 sum = {};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int p = kP - 1; p >= 0; --p)
+                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                w[n][k], __builtin_bit_cast(v8bf16, part[g][n][p]), sum, 0, 0, 0);
+                    const int j = k * 16 + lane / 16 * 4;
+                    auto to = (typename V::T *)b.in + row * b.in_stride + j;
+                    const float y[4] = {sum[0], sum[1], sum[2], sum[3]};
+                    if (b.in_vec) {
+                        if (row < b.rows && j < b.cols) V::put4(to, y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (row < b.rows && j + e < b.cols) V::put(to + e, y[e]);
+                    }
+                }
+            }
+        }
+        wave_fence();
+        if (b.sums || b.bias) {
+            v8bf16 q[KT];
+#pragma unroll
+            for (int k = 0; k < KT; ++k) q[k] = read_columns<kPitchA>(as, k * 16);
+#pragma unroll
+            for (int n = 0; n < 2 * NT; ++n)
+#pragma unroll
+                for (int p = kP - 1; p >= 0; --p) {
+                    const v8bf16 g = read_columns<kPitchG>(gs + p * kStep * kPitchG, n * 16);
+#pragma unroll
+                    for (int k = 0; k < KT; ++k)
+                        acc[n][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[k], g, acc[n][k], 0, 0, 0);
+                    acc_bias[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, g, acc_bias[n], 0, 0, 0);
+                }
+        }
+        wave_fence();
+    }
+    if (!b.sums && !b.bias) return;
+    // the waves' sums, [wave][kN][kK], then their biases [wave][kN]
+    __syncthreads();
+    float *sums = (float *)lds, *bias = sums + kWaves * kN * kK;
+#pragma unroll
+    for (int n = 0; n < 2 * NT; ++n) {
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+            *(v4f32 *)&sums[(wave * kN + n * 16 + lane % 16) * kK + k * 16 + lane / 16 * 4] = acc[n][k];
+        if (lane < 16) bias[wave * kN + n * 16 + lane] = acc_bias[n][0];
+    }
+    __syncthreads();
+    if (b.sums)
+        for (int e = threadIdx.x; e < kN * kK; e += kThreads) {
+            float x = sums[e];
+            for (int v = 1; v < kWaves; ++v) x += sums[v * kN * kK + e];
+            const int n = e / kK, k = e % kK;
+            if (n < b.outs && k < b.cols)
+                b.sums[((int64_t)blockIdx.x * b.outs + n) * b.cols + k] = x;
+        }
+    if (b.bias)
+        for (int n = threadIdx.x; n < b.outs; n += kThreads) {
+            float x = bias[n];
+            for (int v = 1; v < kWaves; ++v) x += bias[v * kN + n];
+            b.bias[(int64_t)blockIdx.x * b.outs + n] = x;
+        }
+}
+
+// to[e] = sum of from[s][e] over the splits s, of two lists; a wave takes every
+// kJoin-th split of 64 elements, and the waves' sums are added in order.
+constexpr int kJoin = 8;
+struct JoinArgs {
+    const float *from[2];
+    float *to[2];
+    int64_t n[2], blocks;   // blocks: of the first list
+    int splits;
+};
+__global__ __launch_bounds__(64 * kJoin) void join(JoinArgs a) {
+    __shared__ double sums[kJoin][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int which = blockIdx.x >= a.blocks;
+    const int64_t n = a.n[which];
+    const int64_t e = ((int64_t)blockIdx.x - (which ? a.blocks : 0)) * 64 + lane;
+    const float *from = a.from[which];
+    double x = 0.0;
+    if (e < n)
+#pragma unroll 4
+        for (int s = wave; s < a.splits; s += kJoin) x += from[s * n + e];
+    sums[wave][lane] = x;
+    __syncthreads();
+    if (wave == 0 && e < n) {
+        for (int k = 1; k < kJoin; ++k) x += sums[k][lane];
+        a.to[which][e] = (float)x;
+    }
+}
+
+constexpr int kLarge = 8, kSmall = 4;   // I and J of the two tile sizes
+
+// Whether a result of i x j values is cut into large tiles: where they fill the card.
+bool large_tiles(int64_t i, int64_t j) {
+    constexpr int64_t kSide = 32 * kLarge;
+    return j > kSide / 2 && ((i + kSide - 1) / kSide) * ((j + kSide - 1) / kSide) >= 192;
+}
+
+// Sizes of the narrow kernel for a layer; nt 0: it is too wide.
+struct Narrow {
+    int nt, kt;
+};
+Narrow narrow_of(int64_t cols, int64_t outs) {
+    const int nt = outs <= 32 ? 1 : outs <= 64 ? 2 : 4;
+    const int kt = cols <= 32 ? 2 : cols <= 64 ? 4 : 8;
+    if (outs > 128 || cols > 128 || nt * kt > 16) return Narrow{0, 0};
+    return Narrow{nt, kt};
 }
 
 // Splits of the rows for grad_weight.
 int splits_of(int64_t rows, int64_t cols, int64_t outs) {
-    const int64_t tiles = ((cols + kTile - 1) / kTile) * ((outs + kTile - 1) / kTile);
-    const int64_t most = (rows + 255) / 256;
-    return (int)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, most));
+    const int64_t most = std::max<int64_t>(1, (rows + 127) / 128);
+    if (narrow_of(cols, outs).nt) return (int)std::min<int64_t>(512, most);
+    const bool large = large_tiles(outs, cols);
+    const int64_t side = 32 * (large ? kLarge : kSmall);
+    const int64_t tiles = ((cols + side - 1) / side) * ((outs + side - 1) / side);
+    return (int)std::min(((large ? 256 : 512) + tiles - 1) / tiles, (most + 1) / 2);
 }
 
 size_t sums_bytes(int64_t splits, int64_t cols, int64_t outs) {
     return (size_t)splits * (size_t)outs * (size_t)(cols + 1) * 4;
 }
 
+template <typename V, bool WEIGHT, int S>
+void run_tiles(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
+    const auto tiles = [](int64_t n) { return (unsigned)((n + 32 * S - 1) / (32 * S)); };
+    const unsigned i = tiles(WEIGHT ? b.outs : b.rows), j = products ? tiles(b.cols) : 1;
+    const dim3 grid = WEIGHT ? dim3(j, i, splits) : dim3(i, j, 1);
+    if (b.vec)
+        backward<V, WEIGHT, S, S, true><<<grid, kThreads, 0, stream>>>(b);
+    else
+        backward<V, WEIGHT, S, S, false><<<grid, kThreads, 0, stream>>>(b);
+}
+
+template <typename V, bool WEIGHT>
+void run(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
+    if (large_tiles(WEIGHT ? b.outs : b.rows, b.cols))
+        run_tiles<V, WEIGHT, kLarge>(b, splits, products, stream);
+    else
+        run_tiles<V, WEIGHT, kSmall>(b, splits, products, stream);
+}
+
+template <typename V, int NT, int KT>
+void run_narrow(const NarrowArgs &b, bool vec, int splits, hipStream_t stream) {
+    if (vec)
+        narrow<V, NT, KT, true><<<splits, kThreads, 0, stream>>>(b);
+    else
+        narrow<V, NT, KT, false><<<splits, kThreads, 0, stream>>>(b);
+}
+
+template <typename V>
+void run_narrow(const NarrowArgs &b, Narrow size, bool vec, int splits, hipStream_t stream) {
+    switch (size.nt * 10 + size.kt) {
+        case 12: return run_narrow<V, 1, 2>(b, vec, splits, stream);
+        case 14: return run_narrow<V, 1, 4>(b, vec, splits, stream);
+        case 18: return run_narrow<V, 1, 8>(b, vec, splits, stream);
+        case 22: return run_narrow<V, 2, 2>(b, vec, splits, stream);
+        case 24: return run_narrow<V, 2, 4>(b, vec, splits, stream);
+        case 28: return run_narrow<V, 2, 8>(b, vec, splits, stream);
+        case 42: return run_narrow<V, 4, 2>(b, vec, splits, stream);
+        default: return run_narrow<V, 4, 4>(b, vec, splits, stream);
+    }
+}
+
 }  // namespace
 
 size_t mx4_backward_bytes(int64_t rows, int64_t cols, int64_t outs) {
+    // as a call of any fewer rows needs, too
     return std::max<size_t>(16, sums_bytes(splits_of(rows, cols, outs), cols, outs));
 }
 
@@ -196,35 +574,55 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
     return with_type(grad_out.dtype, [&](auto type) {
         using V = decltype(type);
         const int64_t rows = a.rows, cols = a.cols, outs = w.rows;
-        BackwardArgs b{};
-        b.grad = grad_out.data;
-        b.stride = grad_out.stride;
-        b.rows = rows;
-        b.outs = (int)outs;
-        b.cols = (int)cols;
-        const auto tiles = [](int64_t n) { return (unsigned)((n + kTile - 1) / kTile); };
-        if (grad_in && rows) {
-            b.q = mx4_view(w);
-            b.out = grad_in->data;
-            b.out_stride = grad_in->stride;
-            backward<V, false><<<dim3(tiles(rows), tiles(cols)), kThreads, 0, stream>>>(b);
+        const auto aligned = [](const octnca_rows &x, int64_t to) {
+            return (uintptr_t)x.data % to == 0 && x.stride * V::kBytes % to == 0;
+        };
+        const bool vec = aligned(grad_out, 16) && outs % 8 == 0;
+        const int splits = splits_of(rows, cols, outs);
+        const Narrow size = narrow_of(cols, outs);
+        float *sums = (float *)workspace;
+        float *bias_sums = sums + (int64_t)splits * outs * cols;
+        if (splits == 1) sums = grad_weight, bias_sums = grad_bias;
+        if (size.nt) {
+            NarrowArgs b{grad_out.data, grad_out.stride, (int)rows, (int)outs, (int)cols,
+                         mx4_view(a), mx4_view(w), nullptr, 0, false, grad_weight ? sums : nullptr,
+                         grad_bias ? bias_sums : nullptr};
+            if (grad_in && rows) {
+                b.in = grad_in->data;
+                b.in_stride = grad_in->stride;
+                b.in_vec = aligned(*grad_in, 4 * V::kBytes) && cols % 4 == 0;
+            }
+            if (b.in || b.sums || b.bias) run_narrow<V>(b, size, vec, splits, stream);
+        } else {
+            BackwardArgs b{};
+            b.grad = grad_out.data;
+            b.stride = grad_out.stride;
+            b.rows = rows;
+            b.outs = (int)outs;
+            b.cols = (int)cols;
+            b.vec = vec;
+            if (grad_in && rows) {
+                b.q = mx4_view(w);
+                b.out = grad_in->data;
+                b.out_stride = grad_in->stride;
+                b.out_vec = aligned(*grad_in, 4 * V::kBytes);
+                run<V, false>(b, 1, true, stream);
+            }
+            if (grad_weight || grad_bias) {
+                b.q = mx4_view(a);
+                b.out = grad_weight ? sums : nullptr;
+                b.out_stride = cols;
+                b.out_vec = cols % 4 == 0 && (uintptr_t)sums % 16 == 0;
+                b.bias = grad_bias ? bias_sums : nullptr;
+                b.per_split = ((rows + splits - 1) / splits + kStep - 1) / kStep * kStep;
+                run<V, true>(b, splits, grad_weight != nullptr, stream);
+            }
         }
-        if (grad_weight || grad_bias) {
-            const int splits = splits_of(rows, cols, outs);
-            b.q = mx4_view(a);
-            b.sums = (float *)workspace;
-            b.bias = grad_bias ? b.sums + (int64_t)splits * outs * cols : nullptr;
-            b.per_split = ((rows + splits - 1) / splits + kStep - 1) / kStep * kStep;
-            backward<V, true><<<dim3(grad_weight ? tiles(cols) : 1, tiles(outs), splits), kThreads,
-                                0, stream>>>(b);
-            const auto blocks = [](int64_t n) {
-                return (unsigned)std::min<int64_t>((n + kThreads - 1) / kThreads, 4096);
-            };
-            if (grad_weight)
-                join<<<blocks(outs * cols), kThreads, 0, stream>>>(b.sums, grad_weight, outs * cols,
-                                                                   splits);
-            if (grad_bias)
-                join<<<blocks(outs), kThreads, 0, stream>>>(b.bias, grad_bias, outs, splits);
+        if (splits > 1 && (grad_weight || grad_bias)) {
+            const int64_t n0 = grad_weight ? outs * cols : 0, n1 = grad_bias ? outs : 0;
+            JoinArgs j{{sums, bias_sums}, {grad_weight, grad_bias}, {n0, n1}, (n0 + 63) / 64,
+                       splits};
+            join<<<(unsigned)(j.blocks + (n1 + 63) / 64), 64 * kJoin, 0, stream>>>(j);
         }
         return hipGetLastError();
     });

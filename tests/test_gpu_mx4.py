@@ -218,13 +218,35 @@ def test_backward(gpu, rows, cols, outs, dtype):
                    zip(first, (layer.grad_weight, layer.grad_bias, grad_in)))
 
 
-def test_backward_parts(gpu):
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,outs,pad", [(300, 3500, 3700, 0), (13001, 1030, 133, 0),
+                                                (500, 3584, 3600, 1)])
+def test_large_backward(gpu, rows, cols, outs, dtype, pad):
+    gen = torch.Generator(device=gpu).manual_seed(rows)
+    g = torch.randn(rows, outs, generator=gen, device=gpu).to(TYPES[dtype])
+    layer = CellLayer(torch.randn(outs, cols, generator=gen, device=gpu),
+                      torch.zeros(outs, device=gpu), rows=rows, train=True)
+    layer.kept.quantise(torch.randn(rows, cols, generator=gen, device=gpu))
+    a, v, gd = values_of(layer.kept), values_of(layer.w), g.double()
+    grad_in, wide = spaced(torch.zeros((rows, cols), dtype=TYPES[dtype], device=gpu), pad)
+    layer.backward(spaced(g, pad)[0], grad_in)
+    want = gd @ v
+    check(grad_in, want, sum_bound(3 * outs, gd.abs() @ v.abs(), want, dtype))
+    want = gd.t() @ a
+    check(layer.grad_weight, want, sum_bound(3 * rows, gd.abs().t() @ a.abs(), want, "f32"))
+    want = gd.sum(0)
+    check(layer.grad_bias, want, sum_bound(rows, gd.abs().sum(0), want, "f32"))
+    assert (wide[:, cols:] == 7).all()
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(900, 70, 50), (900, 200, 150), (300, 3500, 3700)])
+def test_backward_parts(gpu, rows, cols, outs):
     """Each gradient alone gives the bits that all together give."""
-    layer = CellLayer(torch.randn(50, 70, device=gpu), rows=900, train=True)
-    layer.kept.quantise(torch.randn(900, 70, device=gpu))
-    g = torch.randn(900, 50, device=gpu)
-    new = lambda: (torch.full((900, 70), 5.0, device=gpu), torch.full((50, 70), 5.0, device=gpu),
-                   torch.full((50,), 5.0, device=gpu))
+    layer = CellLayer(torch.randn(outs, cols, device=gpu), rows=rows, train=True)
+    layer.kept.quantise(torch.randn(rows, cols, device=gpu))
+    g = torch.randn(rows, outs, device=gpu)
+    new = lambda: (torch.full((rows, cols), 5.0, device=gpu),
+                   torch.full((outs, cols), 5.0, device=gpu), torch.full((outs,), 5.0, device=gpu))
     whole = new()
     call = lambda i, w, b: octnca.octree_nca_mx4_backward(g, layer.kept.struct, layer.w.struct, i,
                                                           w, b, layer.workspace)
