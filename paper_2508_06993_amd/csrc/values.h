@@ -10,6 +10,10 @@
 namespace octnca {
 
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+// 16 bytes at any 2-byte (4-byte) address: one load or store, as global memory takes
+// any alignment here.
+typedef Words4 Words4At2 __attribute__((aligned(2)));
+typedef Words4 Words4At4 __attribute__((aligned(4)));
 
 // Values of type DT (octnca_dtype).  Rounding is to nearest, ties to even.
 template <int DT> struct Values;
