@@ -12,69 +12,121 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int64_t kMaxGrid = int64_t(1) << 23;
 
-// Eight columns of a row from column `col` on, zeros past the last.  VEC: rows
-// start at multiples of 16 bytes.
-template <typename V, bool VEC>
-__device__ __forceinline__ void load_row8(const typename V::T *row, int col, int cols, float *x) {
-    if (VEC && col + 8 <= cols) {
-        V::get8(row + col, x);
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = col + k < cols ? V::get(row + col + k) : 0.0f;
+// x of lane K of each four lanes; of the lane's partner in them.
+template <int K> __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, K * 0x55, 15, 15, true);
+}
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+    x = std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 15, 15, true));
+    return std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 15, 15, true));
 }
 
-// A wave takes a block of a row group: four lanes a row, eight values each.
-template <typename V, bool VEC>
+// A unit is a block of a row group, 256 bytes of codes; a wave takes kUnits in a row.
+// Four lanes have a block of a row, eight columns each; sixteen the same row of all
+// units (with four blocks of a row 256 bytes of fp16 in a row), and a pass of the wave
+// four rows of each unit.
+constexpr int kUnits = 4, kPasses = 4;
+struct Place {
+    int64_t unit, row;   // row: of pass 0; of pass k 4 k more
+    int col;
+};
+__device__ __forceinline__ Place place_of(int64_t first, int blocks) {
+    const int lane = threadIdx.x & 63, unit = lane % 16 / 4;
+    int64_t group = first / blocks;
+    int block = (int)(first - group * blocks) + unit;
+    if (blocks >= kUnits) {
+        if (block >= blocks) block -= blocks, ++group;
+    } else {
+        group += block / blocks;
+        block %= blocks;
+    }
+    return Place{first + unit, group * kMxGroup + lane / 16, block * kMxBlock + lane % 4 * 8};
+}
+
+// NARROW: rows of fewer than eight columns.
+template <typename V, bool NARROW>
 __global__ __launch_bounds__(kThreads) void quantise(const typename V::T *__restrict__ x,
                                                      int64_t stride, int cols, Mx4View m,
                                                      int64_t units) {
     const int lane = threadIdx.x & 63;
-    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); u < units;
-         u += (int64_t)gridDim.x * (kThreads / 64)) {
-        const int64_t group = u / m.blocks;
-        const int block = (int)(u - group * m.blocks);
-        const int64_t row = group * kMxGroup + lane / 4;
-        const bool in = row < m.rows;
-        float v[8];
-        load_row8<V, VEC>(x + (in ? row : m.rows - 1) * stride, block * kMxBlock + lane % 4 * 8,
-                          cols, v);
-        uint32_t top = 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t u = ((int64_t)blockIdx.x * (kThreads / 64) + wave) * kUnits; u < units;
+         u += (int64_t)gridDim.x * (kThreads / 64) * kUnits) {
+        const Place p = place_of(u, m.blocks);
+        Eight<V> raw[kPasses];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) top = std::max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-        top = std::max(top, (uint32_t)__shfl_xor((int)top, 1));
-        top = std::max(top, (uint32_t)__shfl_xor((int)top, 2));
-        const uint32_t scale = mx4_scale(top);
-        const uint32_t c = mx4_codes(v, mx4_inverse(scale));
-        if (in) {
-            ((uint32_t *)m.codes)[u * 64 + lane] = c;
-            if (lane % 4 == 0) m.scales[u * kMxGroup + lane / 4] = (uint8_t)scale;
+        for (int k = 0; k < kPasses; ++k) {
+            const typename V::T *row = x + std::min(p.row + 4 * k, m.rows - 1) * stride;
+            if (NARROW) {
+                raw[k].down = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    raw[k].v[e] = p.col + e < cols ? row[p.col + e] : (typename V::T)0.0f;
+            } else {
+                raw[k].load(row, p.col, cols);
+            }
         }
+        uint32_t scale[kPasses];
+#pragma unroll
+        for (int k = 0; k < kPasses; ++k) {
+            float v[8];
+            raw[k].values(v);
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = std::max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+            scale[k] = mx4_scale(quad_max(top));
+            const uint32_t c = mx4_codes(v, mx4_inverse(scale[k]));
+            if (p.row + 4 * k < m.rows)
+                ((uint32_t *)m.codes)[p.unit * 64 + (4 * k + lane / 16) * 4 + lane % 4] = c;
+        }
+        // lane q of a block's four stores the scale of pass q's row
+        const int q = lane % 4;
+        const uint32_t s = q < 2 ? q == 0 ? scale[0] : scale[1] : q == 2 ? scale[2] : scale[3];
+        if (p.row + 4 * q < m.rows)
+            m.scales[p.unit * kMxGroup + 4 * q + lane / 16] = (uint8_t)s;
     }
 }
 
-template <typename V, bool VEC>
+template <typename V>
 __global__ __launch_bounds__(kThreads) void dequantise(Mx4View m, typename V::T *__restrict__ x,
                                                        int64_t stride, int cols, int64_t units) {
     const int lane = threadIdx.x & 63;
-    for (int64_t u = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); u < units;
-         u += (int64_t)gridDim.x * (kThreads / 64)) {
-        const int64_t group = u / m.blocks;
-        const int col = (int)(u - group * m.blocks) * kMxBlock + lane % 4 * 8;
-        const int64_t row = group * kMxGroup + lane / 4;
-        if (row >= m.rows) continue;
-        float v[8];
-        mx4_values(((const uint32_t *)m.codes)[u * 64 + lane], v);
-        const float scale = mx4_scale_value(m.scales[u * kMxGroup + lane / 4]);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t u = ((int64_t)blockIdx.x * (kThreads / 64) + wave) * kUnits; u < units;
+         u += (int64_t)gridDim.x * (kThreads / 64) * kUnits) {
+        const Place p = place_of(u, m.blocks);
+        const int64_t unit = std::min(p.unit, units - 1);
+        uint32_t c[kPasses];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= scale;
-        typename V::T *to = x + row * stride + col;
-        if (VEC && col + 8 <= cols) {
-            V::put8(to, v);
-        } else {
+        for (int k = 0; k < kPasses; ++k) {
+            const int64_t at = unit * 64 + (4 * k + lane / 16) * 4;
+            if (V::kBytes == 4) {   // fours 4 q and 16 + 4 q: 64 bytes in a row a store
+                const uint16_t *from = (const uint16_t *)((const uint32_t *)m.codes + at);
+                c[k] = from[lane % 4] | (uint32_t)from[4 + lane % 4] << 16;
+            } else {
+                c[k] = ((const uint32_t *)m.codes)[at + lane % 4];
+            }
+        }
+        // lane q of a block's four has the scale of pass q's row
+        const uint32_t s = m.scales[unit * kMxGroup + lane % 4 * 4 + lane / 16];
+        const uint32_t scale[kPasses] = {quad_lane<0>(s), quad_lane<1>(s), quad_lane<2>(s),
+                                         quad_lane<3>(s)};
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (col + k < cols) V::put(to + k, v[k]);
+        for (int k = 0; k < kPasses; ++k) {
+            float v[8];
+            mx4_values(c[k], v);
+            const float factor = mx4_scale_value(scale[k]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= factor;
+            if (p.row + 4 * k >= m.rows) continue;
+            typename V::T *row = x + (p.row + 4 * k) * stride;
+            if (V::kBytes == 4) {
+                const int col = p.col - lane % 4 * 4;
+                if (col < cols) store4<V>(row + col, v, cols - col);
+                if (col + 16 < cols) store4<V>(row + col + 16, v + 4, cols - col - 16);
+            } else if (p.col < cols) {
+                store8<V>(row + p.col, v, cols - p.col);
+            }
         }
     }
 }
@@ -144,12 +196,13 @@ hipError_t launch_mx4_quantise(const octnca_rows &x, const octnca_mx4 &m, hipStr
         using V = decltype(type);
         const Mx4View v = mx4_view(m);
         const int64_t units = (m.rows + kMxGroup - 1) / kMxGroup * v.blocks;
-        const unsigned grid = (unsigned)std::min((units + 3) / 4, kMaxGrid);
+        const int64_t grid = (units + kUnits * 4 - 1) / (kUnits * 4);
         const auto from = (const typename V::T *)x.data;
-        if (rows_aligned(x, 16))
-            quantise<V, true><<<grid, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
+        const unsigned n = (unsigned)std::min(grid, kMaxGrid);
+        if (m.cols < 8)
+            quantise<V, true><<<n, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
         else
-            quantise<V, false><<<grid, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
+            quantise<V, false><<<n, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
         return hipGetLastError();
     });
 }
@@ -159,12 +212,9 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
         using V = decltype(type);
         const Mx4View v = mx4_view(m);
         const int64_t units = (m.rows + kMxGroup - 1) / kMxGroup * v.blocks;
-        const unsigned grid = (unsigned)std::min((units + 3) / 4, kMaxGrid);
-        const auto to = (typename V::T *)x.data;
-        if (rows_aligned(x, 16))
-            dequantise<V, true><<<grid, kThreads, 0, stream>>>(v, to, x.stride, (int)m.cols, units);
-        else
-            dequantise<V, false><<<grid, kThreads, 0, stream>>>(v, to, x.stride, (int)m.cols, units);
+        const int64_t grid = (units + kUnits * 4 - 1) / (kUnits * 4);
+        dequantise<V><<<(unsigned)std::min(grid, kMaxGrid), kThreads, 0, stream>>>(
+            v, (typename V::T *)x.data, x.stride, (int)m.cols, units);
         return hipGetLastError();
     });
 }

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "octree_nca.h"
 
 namespace octnca {
@@ -23,9 +25,8 @@ template <> struct Values<OCTNCA_F32> {
     static constexpr int kBytes = 4;
     static __device__ __forceinline__ float get(const T *p) { return *p; }
     static __device__ __forceinline__ void put(T *p, float x) { *p = x; }
-    // p 16-byte aligned
     static __device__ __forceinline__ void get8(const T *p, float *x) {
-        const Words4 a = ((const Words4 *)p)[0], b = ((const Words4 *)p)[1];
+        const Words4 a = ((const Words4At4 *)p)[0], b = ((const Words4At4 *)p)[1];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             x[k] = __uint_as_float(a[k]);
@@ -39,9 +40,10 @@ template <> struct Values<OCTNCA_F32> {
             a[k] = __float_as_uint(x[k]);
             b[k] = __float_as_uint(x[k + 4]);
         }
-        ((Words4 *)p)[0] = a;
-        ((Words4 *)p)[1] = b;
+        ((Words4At4 *)p)[0] = a;
+        ((Words4At4 *)p)[1] = b;
     }
+    // p 16-byte aligned
     static __device__ __forceinline__ void put4(T *p, const float *x) {
         Words4 a;
 #pragma unroll
@@ -59,7 +61,7 @@ template <typename H> struct Values16 {
     static __device__ __forceinline__ float get(const T *p) { return (float)*p; }
     static __device__ __forceinline__ void put(T *p, float x) { *p = (T)x; }
     static __device__ __forceinline__ void get8(const T *p, float *x) {
-        const H8 a = *(const H8 *)p;
+        const H8 a = __builtin_bit_cast(H8, *(const Words4At2 *)p);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = (float)a[k];
     }
@@ -67,7 +69,7 @@ template <typename H> struct Values16 {
         H8 a;
 #pragma unroll
         for (int k = 0; k < 8; ++k) a[k] = (H)x[k];
-        *(H8 *)p = a;
+        *(Words4At2 *)p = __builtin_bit_cast(Words4, a);
     }
     // p 8-byte aligned
     static __device__ __forceinline__ void put4(T *p, const float *x) {
@@ -79,6 +81,73 @@ template <typename H> struct Values16 {
 };
 template <> struct Values<OCTNCA_F16> : Values16<_Float16> {};
 template <> struct Values<OCTNCA_BF16> : Values16<__bf16> {};
+
+// Eight values from column `col` of a row of `cols` >= 8 on, as loaded: where the row
+// ends before the eighth they are its last eight, and `down` of them come before
+// `col`.
+template <typename V> struct Eight {
+    typename V::T v[8];
+    int down;
+    __device__ __forceinline__ void load(const typename V::T *row, int col, int cols) {
+        down = col + 8 > cols ? col + 8 - cols : 0;
+        using At = std::conditional_t<V::kBytes == 4, Words4At4, Words4At2>;
+        const At *from = (const At *)(row + (col - down));
+        Words4 w[V::kBytes / 2];
+#pragma unroll
+        for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k];
+        __builtin_memcpy(v, w, sizeof(w));
+    }
+    // x = the values, zeros past the row's end
+    __device__ __forceinline__ void values(float *x) const {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = (float)v[k];
+        if (!__any(down)) return;
+#pragma unroll
+        for (int step = 8; step; step /= 2)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float here = x[k], after = k + step < 8 ? x[k + step < 8 ? k + step : k] : 0.0f;
+                x[k] = (step == 8 ? down >= 8 : (down & step) != 0) ? after : here;
+            }
+    }
+};
+
+// Stores the first `left` of eight values (all of them, if more).
+template <typename V>
+__device__ __forceinline__ void store8(typename V::T *to, const float *x, int left) {
+    if (left >= 8) {
+        V::put8(to, x);
+        return;
+    }
+    int k = 0;
+    typename V::T y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (typename V::T)x[e];
+    if (left & 4) {
+        __builtin_memcpy(to, y, 4 * sizeof(y[0]));
+        k = 4;
+    }
+    if (left & 2) {
+        const typename V::T two[2] = {k ? y[4] : y[0], k ? y[5] : y[1]};
+        __builtin_memcpy(to + k, two, sizeof(two));
+        k += 2;
+    }
+    if (left & 1) to[k] = k < 4 ? k ? y[2] : y[0] : k == 4 ? y[4] : y[6];
+}
+
+// Stores the first `left` of four values (all of them, if more).
+template <typename V>
+__device__ __forceinline__ void store4(typename V::T *to, const float *x, int left) {
+    typename V::T y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (typename V::T)x[e];
+    if (left >= 4) {
+        __builtin_memcpy(to, y, sizeof(y));
+        return;
+    }
+    if (left & 2) __builtin_memcpy(to, y, 2 * sizeof(y[0]));
+    if (left & 1) to[left - 1] = left == 1 ? y[0] : y[2];
+}
 
 // Calls f with the type as a constant.
 template <typename F> auto with_type(int32_t dtype, F f) {
