@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void quantise(const typename V::T *__rest
     }
 }
 
-template <typename V>
+template <typename V, bool STREAM>
 __global__ __launch_bounds__(kThreads) void dequantise(Mx4View m, typename V::T *__restrict__ x,
                                                        int64_t stride, int cols, int64_t units) {
     const int lane = threadIdx.x & 63;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void dequantise(Mx4View m, typename V::T 
                 if (col < cols) store4<V>(row + col, v, cols - col);
                 if (col + 16 < cols) store4<V>(row + col + 16, v + 4, cols - col - 16);
             } else if (p.col < cols) {
-                store8<V>(row + p.col, v, cols - p.col);
+                store8<V, STREAM>(row + p.col, v, cols - p.col);
             }
         }
     }
@@ -185,6 +185,14 @@ __global__ __launch_bounds__(kThreads) void product(ProductArgs p) {
             store4<V>(p, row, (tile + t) * kMxGroup + lane / kMxGroup * 4, acc[t]);
 }
 
+// Whether a matrix is so large (half the last-level cache) that its values are written
+// past it.  us through it and past it: 1.2M x 128 fp16 72 and 58, 65536 x 4096 bf16
+// 121 and 111.  Not where a store has less than 128 bytes in a row or lines stay half
+// written: 600 thousand x 100 fp32 71 and 107, 30000 x 4100 fp16 74 and 89.
+bool streams(const octnca_rows &x, int64_t rows, int64_t cols) {
+    return rows * cols * (x.dtype == OCTNCA_F32 ? 4 : 2) >= int64_t(1) << 27;
+}
+
 bool rows_aligned(const octnca_rows &x, int to) {
     return (uintptr_t)x.data % to == 0 && x.stride * (x.dtype == OCTNCA_F32 ? 4 : 2) % to == 0;
 }
@@ -199,10 +207,13 @@ hipError_t launch_mx4_quantise(const octnca_rows &x, const octnca_mx4 &m, hipStr
         const int64_t grid = (units + kUnits * 4 - 1) / (kUnits * 4);
         const auto from = (const typename V::T *)x.data;
         const unsigned n = (unsigned)std::min(grid, kMaxGrid);
+        const auto run = [&](auto kernel) {
+            kernel<<<n, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
+        };
         if (m.cols < 8)
-            quantise<V, true><<<n, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
+            run(quantise<V, true>);
         else
-            quantise<V, false><<<n, kThreads, 0, stream>>>(from, x.stride, (int)m.cols, v, units);
+            run(quantise<V, false>);
         return hipGetLastError();
     });
 }
@@ -213,8 +224,15 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
         const Mx4View v = mx4_view(m);
         const int64_t units = (m.rows + kMxGroup - 1) / kMxGroup * v.blocks;
         const int64_t grid = (units + kUnits * 4 - 1) / (kUnits * 4);
-        dequantise<V><<<(unsigned)std::min(grid, kMaxGrid), kThreads, 0, stream>>>(
-            v, (typename V::T *)x.data, x.stride, (int)m.cols, units);
+        const auto run = [&](auto kernel) {
+            kernel<<<(unsigned)std::min(grid, kMaxGrid), kThreads, 0, stream>>>(
+                v, (typename V::T *)x.data, x.stride, (int)m.cols, units);
+        };
+        const bool whole = x.stride == m.cols && m.cols * V::kBytes % 16 == 0 && rows_aligned(x, 16);
+        if (V::kBytes == 2 && whole && streams(x, m.rows, m.cols))
+            run(dequantise<V, true>);
+        else
+            run(dequantise<V, false>);
         return hipGetLastError();
     });
 }

@@ -33,6 +33,7 @@ template <> struct Values<OCTNCA_F32> {
             x[k + 4] = __uint_as_float(b[k]);
         }
     }
+    template <bool STREAM = false>
     static __device__ __forceinline__ void put8(T *p, const float *x) {
         Words4 a, b;
 #pragma unroll
@@ -65,11 +66,16 @@ template <typename H> struct Values16 {
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = (float)a[k];
     }
+    template <bool STREAM = false>
     static __device__ __forceinline__ void put8(T *p, const float *x) {
         H8 a;
 #pragma unroll
         for (int k = 0; k < 8; ++k) a[k] = (H)x[k];
-        *(Words4At2 *)p = __builtin_bit_cast(Words4, a);
+        const Words4 w = __builtin_bit_cast(Words4, a);
+        if (STREAM)
+            __builtin_nontemporal_store(w, (Words4At2 *)p);
+        else
+            *(Words4At2 *)p = w;
     }
     // p 8-byte aligned
     static __device__ __forceinline__ void put4(T *p, const float *x) {
@@ -113,10 +119,10 @@ template <typename V> struct Eight {
 };
 
 // Stores the first `left` of eight values (all of them, if more).
-template <typename V>
+template <typename V, bool STREAM = false>
 __device__ __forceinline__ void store8(typename V::T *to, const float *x, int left) {
     if (left >= 8) {
-        V::put8(to, x);
+        V::template put8<STREAM>(to, x);
         return;
     }
     int k = 0;
