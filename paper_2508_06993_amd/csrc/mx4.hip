@@ -1,6 +1,7 @@
 // Matrices in microscaled 4 bits: quantisation and product (formulas and layout
 // in octree_nca.h).
 #include <algorithm>
+#include <utility>
 
 #include "launch.h"
 #include "mx4.h"
@@ -142,7 +143,7 @@ struct ProductArgs {
 
 // Outputs n .. n + 3 of a row.
 template <typename V>
-__device__ __forceinline__ void store4(const ProductArgs &p, int64_t row, int n, v4f32 acc) {
+__device__ __forceinline__ void put_outputs(const ProductArgs &p, int64_t row, int n, v4f32 acc) {
     const int outs = (int)p.w.rows;
     float y[4];
 #pragma unroll
@@ -182,7 +183,97 @@ __global__ __launch_bounds__(kThreads) void product(ProductArgs p) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
         if (tile + t < w_groups)
-            store4<V>(p, row, (tile + t) * kMxGroup + lane / kMxGroup * 4, acc[t]);
+            put_outputs<V>(p, row, (tile + t) * kMxGroup + lane / kMxGroup * 4, acc[t]);
+}
+
+// Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
+// them with its sums in registers.  128 columns at a time (four blocks) go through
+// LDS: the next ones are on their way into registers while these are multiplied.
+// Blocks past the last come as codes 0 with scale 1.
+template <typename V, int S>
+__global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row_tiles,
+                                                          int out_tiles) {
+    constexpr int kGroups = 2 * S, kLoads = kGroups / 4;   // row groups of a side
+    __shared__ Words4 codes[2][2][kGroups][64];
+    __shared__ uint32_t scales[2][2][kGroups][16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups go round the eight dies, each with its own L2: a die takes tiles in
+    // a row, which run down eight row tiles before they go to the next outputs.
+    int tile = blockIdx.x;
+    const int each = (int)gridDim.x / 8;
+    if (tile < each * 8) tile = tile % 8 * each + tile / 8;
+    const int band = tile / (8 * out_tiles), deep = std::min(8, row_tiles - band * 8);
+    const int in_band = tile - band * 8 * out_tiles;
+    const int64_t group0[2] = {(int64_t)(band * 8 + in_band % deep) * kGroups,
+                               (int64_t)(in_band / deep) * kGroups};
+    const Mx4View side[2] = {p.a, p.w};
+    const int blocks = p.a.blocks;
+
+    Words4 next[2][kLoads];
+    uint32_t next_scales[2];
+    const auto load = [&](int block) {
+        const bool in = block + lane / kMxGroup < blocks;
+        const uint32_t mask = in ? ~0u : 0u;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int64_t last = (side[s].rows + kMxGroup - 1) / kMxGroup - 1;
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                const int64_t group = std::min(group0[s] + k * 4 + wave, last);
+                const Words4 *from = (const Words4 *)side[s].codes + (group * blocks + block) * kMxGroup;
+                next[s][k] = from[in ? lane : 0] & mask;
+            }
+            // a thread takes four rows' scales of a block
+            const int part = threadIdx.x % 16;
+            const bool there = block + part / 4 < blocks && threadIdx.x < kGroups * 16;
+            const int64_t group = std::min(group0[s] + (int)threadIdx.x / 16, last);
+            const uint32_t *from = (const uint32_t *)side[s].scales + (group * blocks + block) * 4;
+            next_scales[s] = there ? from[there ? part : 0] : 0x7f7f7f7fu;
+        }
+    };
+    const auto store = [&](int buffer) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) codes[buffer][s][k * 4 + wave][lane] = next[s][k];
+            if (kGroups == 16 || threadIdx.x < kGroups * 16)
+                scales[buffer][s][threadIdx.x / 16][threadIdx.x % 16] = next_scales[s];
+        }
+    };
+    const auto operand = [&](int buffer, int s, int group) {
+        return Mx4Operand{codes[buffer][s][group][lane],
+                          ((const uint8_t *)scales[buffer][s][group])[lane]};
+    };
+    v4f32 acc[S][S] = {};
+    load(0);
+    store(0);
+    int buffer = 0;
+    const int ga = wave % 2 * S, gw = wave / 2 * S;
+    for (int block = 0; block < blocks; block += 4, buffer ^= 1) {
+        __syncthreads();
+        load(std::min(block + 4, blocks - 1));   // past the end: used by no one
+        Mx4Operand w[S];
+#pragma unroll
+        for (int t = 0; t < S; ++t) w[t] = operand(buffer, 1, gw + t);
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const Mx4Operand a = operand(buffer, 0, ga + i);
+#pragma unroll
+            for (int t = 0; t < S; ++t) acc[i][t] = mx4_mfma(w[t], a, acc[i][t]);
+        }
+        store(buffer ^ 1);
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const int64_t row = (group0[0] + ga + i) * kMxGroup + lane % kMxGroup;
+        if (row >= p.a.rows) continue;
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const int64_t n = (group0[1] + gw + t) * kMxGroup + lane / kMxGroup * 4;
+            if (n < p.w.rows) put_outputs<V>(p, row, (int)n, acc[i][t]);
+        }
+    }
 }
 
 // Whether a matrix is so large (half the last-level cache) that its values are written
@@ -243,6 +334,20 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
         using V = decltype(type);
         const ProductArgs p{mx4_view(a), mx4_view(w), bias, relu, out.data, out.stride,
                             rows_aligned(out, 4 * V::kBytes)};
+        const auto tiles_of = [&](int side) {
+            return std::make_pair((a.rows + side - 1) / side, (w.rows + side - 1) / side);
+        };
+        const auto large = tiles_of(256), small = tiles_of(128);
+        if (large.first * large.second >= 192) {
+            product_tiles<V, 8><<<(unsigned)(large.first * large.second), kThreads, 0, stream>>>(
+                p, (int)large.first, (int)large.second);
+            return hipGetLastError();
+        }
+        if (small.first * small.second >= 128) {
+            product_tiles<V, 4><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
+                p, (int)small.first, (int)small.second);
+            return hipGetLastError();
+        }
         const int64_t groups = (a.rows + kMxGroup - 1) / kMxGroup;
         const int64_t tiles = (w.rows + kMxGroup * kTiles - 1) / (kMxGroup * kTiles);
         product<V><<<dim3((unsigned)((groups + 3) / 4), (unsigned)tiles), kThreads, 0, stream>>>(p);
