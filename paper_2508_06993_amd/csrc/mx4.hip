@@ -189,13 +189,16 @@ __global__ __launch_bounds__(kThreads) void product(ProductArgs p) {
 // Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
 // them with its sums in registers.  128 columns at a time (four blocks) go through
 // LDS: the next ones are on their way into registers while these are multiplied.
-// Blocks past the last come as codes 0 with scale 1.
+// Blocks past the last come as codes 0 with scale 1.  The weights' rows go to the
+// operands so that a lane ends up with 4 S outputs in a row of one row.
 template <typename V, int S>
 __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row_tiles,
                                                           int out_tiles) {
     constexpr int kGroups = 2 * S, kLoads = kGroups / 4;   // row groups of a side
-    __shared__ Words4 codes[2][2][kGroups][64];
-    __shared__ uint32_t scales[2][2][kGroups][16];
+    // rows 4 S apart are read together: after each group a part of the banks is skipped
+    constexpr int kPitch = 64 + 16 / S;
+    __shared__ Words4 codes[2][2][kGroups * kPitch];
+    __shared__ uint32_t scales[2][2][kGroups * 16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go round the eight dies, each with its own L2: a die takes tiles in
@@ -212,9 +215,11 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
 
     Words4 next[2][kLoads];
     uint32_t next_scales[2];
+    bool next_in, next_scales_in;   // applied when the values are stored: no wait before
     const auto load = [&](int block) {
-        const bool in = block + lane / kMxGroup < blocks;
-        const uint32_t mask = in ? ~0u : 0u;
+        next_in = block + lane / kMxGroup < blocks;
+        const int part = threadIdx.x % 16;   // a thread takes four rows' scales of a block
+        next_scales_in = block + part / 4 < blocks;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int64_t last = (side[s].rows + kMxGroup - 1) / kMxGroup - 1;
@@ -222,56 +227,76 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
             for (int k = 0; k < kLoads; ++k) {
                 const int64_t group = std::min(group0[s] + k * 4 + wave, last);
                 const Words4 *from = (const Words4 *)side[s].codes + (group * blocks + block) * kMxGroup;
-                next[s][k] = from[in ? lane : 0] & mask;
+                next[s][k] = from[next_in ? lane : 0];
             }
-            // a thread takes four rows' scales of a block
-            const int part = threadIdx.x % 16;
-            const bool there = block + part / 4 < blocks && threadIdx.x < kGroups * 16;
             const int64_t group = std::min(group0[s] + (int)threadIdx.x / 16, last);
             const uint32_t *from = (const uint32_t *)side[s].scales + (group * blocks + block) * 4;
-            next_scales[s] = there ? from[there ? part : 0] : 0x7f7f7f7fu;
+            next_scales[s] = from[next_scales_in ? part : 0];
         }
     };
     const auto store = [&](int buffer) {
+        const uint32_t mask = next_in ? ~0u : 0u;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int k = 0; k < kLoads; ++k) codes[buffer][s][k * 4 + wave][lane] = next[s][k];
+            for (int k = 0; k < kLoads; ++k)
+                codes[buffer][s][(k * 4 + wave) * kPitch + lane] = next[s][k] & mask;
             if (kGroups == 16 || threadIdx.x < kGroups * 16)
-                scales[buffer][s][threadIdx.x / 16][threadIdx.x % 16] = next_scales[s];
+                scales[buffer][s][threadIdx.x] = next_scales_in ? next_scales[s] : 0x7f7f7f7fu;
         }
     };
-    const auto operand = [&](int buffer, int s, int group) {
-        return Mx4Operand{codes[buffer][s][group][lane],
-                          ((const uint8_t *)scales[buffer][s][group])[lane]};
+    const int ga = wave % 2 * S, gw = wave / 2 * S;
+    const auto row_operand = [&](int buffer, int i) {
+        return Mx4Operand{codes[buffer][0][(ga + i) * kPitch + lane],
+                          ((const uint8_t *)scales[buffer][0])[(ga + i) * 64 + lane]};
+    };
+    const auto out_operand = [&](int buffer, int t) {
+        const int n = lane % 16 / 4 * (4 * S) + t * 4 + lane % 4;   // of the wave's outputs
+        const int group = gw + n / 16, at = lane / 16 * 16 + n % 16;
+        return Mx4Operand{codes[buffer][1][group * kPitch + at],
+                          ((const uint8_t *)scales[buffer][1])[group * 64 + at]};
     };
     v4f32 acc[S][S] = {};
     load(0);
     store(0);
     int buffer = 0;
-    const int ga = wave % 2 * S, gw = wave / 2 * S;
     for (int block = 0; block < blocks; block += 4, buffer ^= 1) {
         __syncthreads();
         load(std::min(block + 4, blocks - 1));   // past the end: used by no one
-        Mx4Operand w[S];
+        Mx4Operand w[S], a = row_operand(buffer, 0);
 #pragma unroll
-        for (int t = 0; t < S; ++t) w[t] = operand(buffer, 1, gw + t);
+        for (int t = 0; t < S; ++t) w[t] = out_operand(buffer, t);
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            const Mx4Operand a = operand(buffer, 0, ga + i);
+            const Mx4Operand after = row_operand(buffer, i + 1 < S ? i + 1 : i);
+            __builtin_amdgcn_sched_barrier(0);   // on its way during these
 #pragma unroll
             for (int t = 0; t < S; ++t) acc[i][t] = mx4_mfma(w[t], a, acc[i][t]);
+            a = after;
         }
+        __builtin_amdgcn_sched_barrier(0);
         store(buffer ^ 1);
     }
+    // 4 S outputs of row lane % 16 of each group, from n on
+    const int64_t n = (group0[1] + gw) * kMxGroup + lane / 16 * (4 * S);
+    const int left = (int)std::min<int64_t>(std::max<int64_t>(p.w.rows - n, 0), 4 * S);
+    float bias[4 * S];
+#pragma unroll
+    for (int k = 0; k < 4 * S; ++k) bias[k] = p.bias && k < left ? p.bias[n + k] : 0.0f;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
         const int64_t row = (group0[0] + ga + i) * kMxGroup + lane % kMxGroup;
         if (row >= p.a.rows) continue;
+        typename V::T *to = (typename V::T *)p.out + row * p.stride + n;
 #pragma unroll
-        for (int t = 0; t < S; ++t) {
-            const int64_t n = (group0[1] + gw + t) * kMxGroup + lane / kMxGroup * 4;
-            if (n < p.w.rows) put_outputs<V>(p, row, (int)n, acc[i][t]);
+        for (int t = 0; t < S; t += 2) {
+            float y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                y[k] = acc[i][t + k / 4][k % 4] + bias[t * 4 + k];
+                if (p.relu && y[k] < 0.0f) y[k] = 0.0f;
+            }
+            if (left > t * 4) store8<V>(to + t * 4, y, left - t * 4);
         }
     }
 }

@@ -73,25 +73,26 @@ __device__ __forceinline__ v8bf16 read_columns(const uint16_t *tile, int col) {
 // Eight values of G as loaded, ahead of their use.
 template <typename V> struct Raw8 {
     Words4 w[V::kBytes / 2];
+    bool in;   // VEC: whether they count; applied with their use, no wait before
     // Columns col .. col + 7 of a row of `end` (zeros past it, and everywhere where
-    // `in` is false; the row can be read all the same).  No branches: what lies
+    // `row_in` is false; the row can be read all the same).  No branches: what lies
     // outside is read from the row's last columns and replaced.  VEC: rows are
     // aligned, of a multiple of eight columns.
     template <bool VEC>
     __device__ __forceinline__ void load(const typename V::T *row, int64_t col, int64_t end,
-                                         bool in) {
+                                         bool row_in) {
         if (VEC) {
-            const bool all = in && col < end;
+            in = row_in && col < end;
             const Words4 *from = (const Words4 *)(row + (col < end ? col : 0));
-            const uint32_t mask = all ? ~0u : 0u;
 #pragma unroll
-            for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k] & mask;
+            for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k];
         } else {
+            in = true;
             typename V::T x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 x[k] = row[col + k < end ? col + k : end - 1];
-                if (!in || col + k >= end) x[k] = (typename V::T)0.0f;
+                if (!row_in || col + k >= end) x[k] = (typename V::T)0.0f;
             }
             __builtin_memcpy(w, x, sizeof(w));
         }
@@ -100,12 +101,12 @@ template <typename V> struct Raw8 {
         typename V::T v[8];
         __builtin_memcpy(v, w, sizeof(w));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = (float)v[k];
+        for (int k = 0; k < 8; ++k) x[k] = in ? (float)v[k] : 0.0f;
     }
     // part p of the eight, packed
     template <int P> __device__ __forceinline__ void parts(Words4 *out) const {
         if (P == 1) {   // bf16 as it is
-            out[0] = w[0];
+            out[0] = w[0] & (in ? ~0u : 0u);
             return;
         }
         float x[8];
@@ -161,6 +162,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
 
     Raw8<V> p[kLoadsP];
     uint32_t codes[kLoadsQ], scales[kLoadsQ];
+    bool codes_in[kLoadsQ];
     // where a thread's part k of P lies: row and first column of the tile
     const auto p_row = [&](int k) {
         return WEIGHT ? (threadIdx.x + k * kThreads) / (kBi / 8) : threadIdx.x / 4 + k * 64;
@@ -181,13 +183,12 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
         for (int k = 0; k < kLoadsQ; ++k) {
             const int unit = k * 4 + wave, block = j0 / kMxBlock + unit / 2;
             const int64_t c = c0 + unit % 2 * kMxGroup + lane / 4;
-            const bool in = c < c_end && block < b.q.blocks;
+            codes_in[k] = c < c_end && block < b.q.blocks;
             const int64_t row = std::min(c, c_end - 1);
             const int64_t at = (row / kMxGroup * b.q.blocks + std::min(block, b.q.blocks - 1)) *
                                    kMxGroup + row % kMxGroup;
             codes[k] = ((const uint32_t *)b.q.codes)[at * 4 + lane % 4];
             scales[k] = b.q.scales[at];
-            if (!in) codes[k] = 0, scales[k] = 127;
         }
     };
     float bias[8] = {};
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
             const int unit = k * 4 + wave;
             *(Words4 *)&qs[buffer][(unit % 2 * kMxGroup + lane / 4) * kPitchQ +
                                    unit / 2 * kMxBlock + lane % 4 * 8] =
-                code_values(codes[k], scales[k]);
+                code_values(codes_in[k] ? codes[k] : 0, codes_in[k] ? scales[k] : 127);
         }
     };
 
@@ -225,21 +226,26 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     for (int64_t c0 = c_begin; c0 < c_end; c0 += kStep, buffer ^= 1) {
         __syncthreads();
         load(c0 + kStep);   // past the end: zeros, used by no one
-        v8bf16 q[J];
+        const auto operand = [&](int u) {   // part u % kP of rows u / kP
+            const uint16_t *tile = ps[buffer][u % kP];
+            const int row = wi + u / kP * 16;
+            return WEIGHT ? read_columns<kPitchP>(tile, row)
+                          : *(const v8bf16 *)&tile[(row + lane % 16) * kPitchP + lane / 16 * 8];
+        };
+        v8bf16 q[J], g = operand(0);
 #pragma unroll
         for (int t = 0; t < J; ++t) q[t] = read_columns<kPitchQ>(qs[buffer], wj + t * 16);
 #pragma unroll
-        for (int s = 0; s < I; ++s)
+        for (int u = 0; u < I * kP; ++u) {
+            const v8bf16 after = operand(u + 1 < I * kP ? u + 1 : u);
+            __builtin_amdgcn_sched_barrier(0);   // on its way during these
 #pragma unroll
-            for (int k = kP - 1; k >= 0; --k) {
-                const v8bf16 g =
-                    WEIGHT ? read_columns<kPitchP>(ps[buffer][k], wi + s * 16)
-                           : *(const v8bf16 *)&ps[buffer][k][(wi + s * 16 + lane % 16) * kPitchP +
-                                                             lane / 16 * 8];
-#pragma unroll
-                for (int t = 0; t < J; ++t)
-                    acc[s][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t], g, acc[s][t], 0, 0, 0);
-            }
+            for (int t = 0; t < J; ++t)
+                acc[u / kP][t] =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t], g, acc[u / kP][t], 0, 0, 0);
+            g = after;
+        }
+        __builtin_amdgcn_sched_barrier(0);
         store(buffer ^ 1);
     }
     // a lane has four columns j of row i
@@ -342,6 +348,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
 
     Raw8<V> raw[2][NT];
     uint32_t codes[2][kB], scales[2][kB];
+    bool codes_in[2][kB];
     const auto load = [&](int step) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -358,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
                                        kMxGroup + r % kMxGroup;
                 codes[g][k] = ((const uint32_t *)b.a.codes)[at * 4 + lane % 4];
                 scales[g][k] = b.a.scales[at];
-                if (arow >= b.rows || k >= b.a.blocks) codes[g][k] = 0, scales[g][k] = 127;
+                codes_in[g][k] = arow < b.rows && k < b.a.blocks;
             }
         }
     };
@@ -384,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
 #pragma unroll
             for (int k = 0; k < kB; ++k)
                 *(Words4 *)&as[(g * kMxGroup + lane / 4) * kPitchA + k * kMxBlock + lane % 4 * 8] =
-                    code_values(codes[g][k], scales[g][k]);
+                    code_values(codes_in[g][k] ? codes[g][k] : 0, codes_in[g][k] ? scales[g][k] : 127);
         }
         load(step + all);   // past the end: zeros, used by no one
         if (b.in) {
