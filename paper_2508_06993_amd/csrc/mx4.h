@@ -99,4 +99,16 @@ __device__ __forceinline__ v4f32 mx4_mfma(const Mx4Operand &a, const Mx4Operand 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, a.scale, 0, b.scale);
 }
 
+// The same with 32 rows each and two blocks (64 columns): lane l of an operand has row
+// l % 32, block l / 32; acc[i] of lane l is that of a's row 8 (i / 4) + 4 (l / 32) + i % 4
+// and b's row l % 32.  About 1.5 times the rate of the other: with nothing but these
+// instructions in a kernel 9.0 PFLOP/s and 5.4 of the other (one wave a SIMD; 7.0 and
+// 5.2 with random codes).
+typedef float v16f32 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ v16f32 mx4_mfma32(const Mx4Operand &a, const Mx4Operand &b, v16f32 acc) {
+    const v8i32 x = {(int)a.codes[0], (int)a.codes[1], (int)a.codes[2], (int)a.codes[3], 0, 0, 0, 0};
+    const v8i32 y = {(int)b.codes[0], (int)b.codes[1], (int)b.codes[2], (int)b.codes[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 4, 4, 0, a.scale, 0, b.scale);
+}
+
 }  // namespace octnca

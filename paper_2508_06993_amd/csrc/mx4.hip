@@ -188,17 +188,17 @@ __global__ __launch_bounds__(kThreads) void product(ProductArgs p) {
 
 // Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
 // them with its sums in registers.  128 columns at a time (four blocks) go through
-// LDS: the next ones are on their way into registers while these are multiplied.
-// Blocks past the last come as codes 0 with scale 1.  The weights' rows go to the
-// operands so that a lane ends up with 4 S outputs in a row of one row.
-template <typename V, int S>
+// LDS, loaded two steps ahead of their use: one step's products take about half of
+// the time that a load takes to come back.  Blocks past the last come as codes 0 with
+// scale 1.  The weights' rows go to the operands so that a lane ends up with 16 bytes of
+// outputs in a row, and the four lanes of a row with 64.
+template <typename V, int S, int U>
 __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row_tiles,
                                                           int out_tiles) {
     constexpr int kGroups = 2 * S, kLoads = kGroups / 4;   // row groups of a side
-    // rows 4 S apart are read together: after each group a part of the banks is skipped
-    constexpr int kPitch = 64 + 16 / S;
-    __shared__ Words4 codes[2][2][kGroups * kPitch];
-    __shared__ uint32_t scales[2][2][kGroups * 16];
+    constexpr int kEach = 16 / V::kBytes;                  // outputs of a lane in a row
+    __shared__ Words4 codes[2][U][2][kGroups][64];
+    __shared__ uint32_t scales[2][U][2][kGroups][16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go round the eight dies, each with its own L2: a die takes tiles in
@@ -213,13 +213,16 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
     const Mx4View side[2] = {p.a, p.w};
     const int blocks = p.a.blocks;
 
-    Words4 next[2][kLoads];
-    uint32_t next_scales[2];
-    bool next_in, next_scales_in;   // applied when the values are stored: no wait before
-    const auto load = [&](int block) {
-        next_in = block + lane / kMxGroup < blocks;
+    struct Next {
+        Words4 codes[2][kLoads];
+        uint32_t scales[2];
+        bool codes_in, scales_in;   // applied when the values are stored: no wait before
+    };
+    const auto load = [&](Next &x, int from_block) {
+        const int block = std::min(from_block, blocks - 1);
         const int part = threadIdx.x % 16;   // a thread takes four rows' scales of a block
-        next_scales_in = block + part / 4 < blocks;
+        x.codes_in = from_block + lane / kMxGroup < blocks;
+        x.scales_in = from_block + part / 4 < blocks;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int64_t last = (side[s].rows + kMxGroup - 1) / kMxGroup - 1;
@@ -227,77 +230,115 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
             for (int k = 0; k < kLoads; ++k) {
                 const int64_t group = std::min(group0[s] + k * 4 + wave, last);
                 const Words4 *from = (const Words4 *)side[s].codes + (group * blocks + block) * kMxGroup;
-                next[s][k] = from[next_in ? lane : 0];
+                x.codes[s][k] = from[x.codes_in ? lane : 0];
             }
             const int64_t group = std::min(group0[s] + (int)threadIdx.x / 16, last);
             const uint32_t *from = (const uint32_t *)side[s].scales + (group * blocks + block) * 4;
-            next_scales[s] = from[next_scales_in ? part : 0];
+            x.scales[s] = from[x.scales_in ? part : 0];
         }
     };
-    const auto store = [&](int buffer) {
-        const uint32_t mask = next_in ? ~0u : 0u;
+    // Where row r of a group goes: the weights' bits 2 and 3 change places where a lane
+    // is to have eight outputs in a row.
+    const auto place = [&](int s, int r) {
+        return s == 0 || kEach == 4 ? r : (r & 3) | (r & 4) << 1 | (r & 8) >> 1;
+    };
+    // Codes k of a side; past the end zeros of one side do, with scales that are numbers.
+    const auto store_codes = [&](const Next &x, int buffer, int u, int s, int k) {
+        const int at = lane / kMxGroup * kMxGroup + place(s, lane % kMxGroup);
+        codes[buffer][u][s][k * 4 + wave][at] =
+            s == 0 ? x.codes[s][k] & (x.codes_in ? ~0u : 0u) : x.codes[s][k];
+    };
+    const auto store_scales = [&](const Next &x, int buffer, int u) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k)
-                codes[buffer][s][(k * 4 + wave) * kPitch + lane] = next[s][k] & mask;
+            const int at = threadIdx.x % 16 / 4 * 4 + place(s, threadIdx.x % 4 * 4) / 4;
             if (kGroups == 16 || threadIdx.x < kGroups * 16)
-                scales[buffer][s][threadIdx.x] = next_scales_in ? next_scales[s] : 0x7f7f7f7fu;
+                scales[buffer][u][s][threadIdx.x / 16][at] = x.scales_in ? x.scales[s] : 0x7f7f7f7fu;
         }
     };
+    constexpr int kT = S / 2;   // tiles of 32 of a wave, each way
     const int ga = wave % 2 * S, gw = wave / 2 * S;
-    const auto row_operand = [&](int buffer, int i) {
-        return Mx4Operand{codes[buffer][0][(ga + i) * kPitch + lane],
-                          ((const uint8_t *)scales[buffer][0])[(ga + i) * 64 + lane]};
+    const auto operand = [&](int buffer, int u, int s, int group, int half) {
+        const int g = group + lane % 32 / 16, at = (2 * half + lane / 32) * 16 + lane % 16;
+        return Mx4Operand{codes[buffer][u][s][g][at],
+                          ((const uint8_t *)scales[buffer][u][s][g])[at]};
     };
-    const auto out_operand = [&](int buffer, int t) {
-        const int n = lane % 16 / 4 * (4 * S) + t * 4 + lane % 4;   // of the wave's outputs
-        const int group = gw + n / 16, at = lane / 16 * 16 + n % 16;
-        return Mx4Operand{codes[buffer][1][group * kPitch + at],
-                          ((const uint8_t *)scales[buffer][1])[group * 64 + at]};
+    v16f32 acc[kT][kT] = {};
+    Next next[U];
+    // Piece x of what is stored for the next step
+    constexpr int kPieces = U * (2 * kLoads + 1), kTurns = U * 2 * kT;
+    const auto store = [&](int buffer, int x) {
+        const int u = x / (2 * kLoads + 1), piece = x % (2 * kLoads + 1);
+        if (piece < 2 * kLoads)
+            store_codes(next[u], buffer, u, piece / kLoads, piece % kLoads);
+        else
+            store_scales(next[u], buffer, u);
     };
-    v4f32 acc[S][S] = {};
-    load(0);
-    store(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(next[u], 4 * u);
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) store(0, x);
     int buffer = 0;
-    for (int block = 0; block < blocks; block += 4, buffer ^= 1) {
+    for (int block = 0; block < blocks; block += 4 * U, buffer ^= 1) {
         __syncthreads();
-        load(std::min(block + 4, blocks - 1));   // past the end: used by no one
-        Mx4Operand w[S], a = row_operand(buffer, 0);
 #pragma unroll
-        for (int t = 0; t < S; ++t) w[t] = out_operand(buffer, t);
+        for (int u = 0; u < U; ++u) load(next[u], block + 4 * (U + u));
+        // kT products at a time, with the next rows on their way from LDS; in the second
+        // half of them what has been loaded goes there
+        Mx4Operand w[kT], a;
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-            const Mx4Operand after = row_operand(buffer, i + 1 < S ? i + 1 : i);
-            __builtin_amdgcn_sched_barrier(0);   // on its way during these
+        for (int turn = 0; turn < kTurns; ++turn) {
+            const int u = turn / (2 * kT), half = turn / kT % 2, i = turn % kT;
+            if (i == 0) {
+                a = operand(buffer, u, 0, ga, half);
 #pragma unroll
-            for (int t = 0; t < S; ++t) acc[i][t] = mx4_mfma(w[t], a, acc[i][t]);
+                for (int t = 0; t < kT; ++t) w[t] = operand(buffer, u, 1, gw + 2 * t, half);
+            }
+            const Mx4Operand after = operand(buffer, u, 0, ga + 2 * (i + 1 < kT ? i + 1 : i), half);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < kT; ++t) acc[i][t] = mx4_mfma32(w[t], a, acc[i][t]);
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x)
+                if (kTurns / 2 + x * (kTurns / 2) / kPieces == turn) store(buffer ^ 1, x);
             a = after;
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        store(buffer ^ 1);
     }
-    // 4 S outputs of row lane % 16 of each group, from n on
-    const int64_t n = (group0[1] + gw) * kMxGroup + lane / 16 * (4 * S);
-    const int left = (int)std::min<int64_t>(std::max<int64_t>(p.w.rows - n, 0), 4 * S);
-    float bias[4 * S];
+    // kEach outputs of row lane % 32 of each tile, from n on; the next ones 2 kEach on
+    constexpr int kRuns = 16 / kEach;
+    const int64_t n = (group0[1] + gw) * kMxGroup + lane / 32 * kEach;
+    float bias[kT][16];
 #pragma unroll
-    for (int k = 0; k < 4 * S; ++k) bias[k] = p.bias && k < left ? p.bias[n + k] : 0.0f;
+    for (int t = 0; t < kT; ++t)
 #pragma unroll
-    for (int i = 0; i < S; ++i) {
-        const int64_t row = (group0[0] + ga + i) * kMxGroup + lane % kMxGroup;
+        for (int k = 0; k < 16; ++k) {
+            const int64_t at = n + t * 32 + k / kEach * (2 * kEach) + k % kEach;
+            bias[t][k] = p.bias ? p.bias[std::min(at, p.w.rows - 1)] : 0.0f;
+        }
+#pragma unroll
+    for (int i = 0; i < kT; ++i) {
+        const int64_t row = (group0[0] + ga + 2 * i) * kMxGroup + lane % 32;
         if (row >= p.a.rows) continue;
         typename V::T *to = (typename V::T *)p.out + row * p.stride + n;
 #pragma unroll
-        for (int t = 0; t < S; t += 2) {
-            float y[8];
+        for (int t = 0; t < kT; ++t)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                y[k] = acc[i][t + k / 4][k % 4] + bias[t * 4 + k];
-                if (p.relu && y[k] < 0.0f) y[k] = 0.0f;
+            for (int r = 0; r < kRuns; ++r) {
+                float y[kEach];
+#pragma unroll
+                for (int k = 0; k < kEach; ++k) {
+                    y[k] = acc[i][t][r * kEach + k] + bias[t][r * kEach + k];
+                    if (p.relu && y[k] < 0.0f) y[k] = 0.0f;
+                }
+                const int off = t * 32 + r * 2 * kEach;
+                const int64_t left = p.w.rows - n - off;
+                if (left <= 0) continue;
+                if constexpr (kEach == 8)
+                    store8<V>(to + off, y, (int)std::min<int64_t>(left, 8));
+                else
+                    store4<V>(to + off, y, (int)std::min<int64_t>(left, 4));
             }
-            if (left > t * 4) store8<V>(to + t * 4, y, left - t * 4);
-        }
     }
 }
 
@@ -364,12 +405,12 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
         };
         const auto large = tiles_of(256), small = tiles_of(128);
         if (large.first * large.second >= 192) {
-            product_tiles<V, 8><<<(unsigned)(large.first * large.second), kThreads, 0, stream>>>(
+            product_tiles<V, 8, 2><<<(unsigned)(large.first * large.second), kThreads, 0, stream>>>(
                 p, (int)large.first, (int)large.second);
             return hipGetLastError();
         }
         if (small.first * small.second >= 128) {
-            product_tiles<V, 4><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
+            product_tiles<V, 4, 2><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
                 p, (int)small.first, (int)small.second);
             return hipGetLastError();
         }
