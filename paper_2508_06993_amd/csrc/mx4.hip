@@ -218,22 +218,23 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
         uint32_t scales[2];
         bool codes_in, scales_in;   // applied when the values are stored: no wait before
     };
-    const auto load = [&](Next &x, int from_block) {
-        const int block = std::min(from_block, blocks - 1);
-        const int part = threadIdx.x % 16;   // a thread takes four rows' scales of a block
+    const int last[2] = {(int)((p.a.rows + kMxGroup - 1) / kMxGroup) - 1,
+                         (int)((p.w.rows + kMxGroup - 1) / kMxGroup) - 1};
+    const auto load_codes = [&](Next &x, int from_block, int s, int k) {
         x.codes_in = from_block + lane / kMxGroup < blocks;
+        const int64_t group = std::min((int)group0[s] + k * 4 + wave, last[s]);
+        const Words4 *from = (const Words4 *)side[s].codes +
+                             (group * blocks + std::min(from_block, blocks - 1)) * kMxGroup;
+        x.codes[s][k] = from[x.codes_in ? lane : 0];
+    };
+    const auto load_scales = [&](Next &x, int from_block) {
+        const int part = threadIdx.x % 16;   // a thread takes four rows' scales of a block
         x.scales_in = from_block + part / 4 < blocks;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int64_t last = (side[s].rows + kMxGroup - 1) / kMxGroup - 1;
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k) {
-                const int64_t group = std::min(group0[s] + k * 4 + wave, last);
-                const Words4 *from = (const Words4 *)side[s].codes + (group * blocks + block) * kMxGroup;
-                x.codes[s][k] = from[x.codes_in ? lane : 0];
-            }
-            const int64_t group = std::min(group0[s] + (int)threadIdx.x / 16, last);
-            const uint32_t *from = (const uint32_t *)side[s].scales + (group * blocks + block) * 4;
+            const int64_t group = std::min((int)group0[s] + (int)threadIdx.x / 16, last[s]);
+            const uint32_t *from = (const uint32_t *)side[s].scales +
+                                   (group * blocks + std::min(from_block, blocks - 1)) * 4;
             x.scales[s] = from[x.scales_in ? part : 0];
         }
     };
@@ -265,8 +266,15 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
     };
     v16f32 acc[kT][kT] = {};
     Next next[U];
-    // Piece x of what is stored for the next step
+    // Piece x of what is loaded and stored for the next step
     constexpr int kPieces = U * (2 * kLoads + 1), kTurns = U * 2 * kT;
+    const auto load = [&](int block, int x) {
+        const int u = x / (2 * kLoads + 1), piece = x % (2 * kLoads + 1);
+        if (piece < 2 * kLoads)
+            load_codes(next[u], block + 4 * u, piece / kLoads, piece % kLoads);
+        else
+            load_scales(next[u], block + 4 * u);
+    };
     const auto store = [&](int buffer, int x) {
         const int u = x / (2 * kLoads + 1), piece = x % (2 * kLoads + 1);
         if (piece < 2 * kLoads)
@@ -275,32 +283,37 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
             store_scales(next[u], buffer, u);
     };
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(next[u], 4 * u);
+    for (int x = 0; x < kPieces; ++x) load(0, x);
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) store(0, x);
     int buffer = 0;
     for (int block = 0; block < blocks; block += 4 * U, buffer ^= 1) {
         __syncthreads();
+        // kT products a turn, with the next operands on their way from LDS.  The next
+        // step's pieces are loaded in the first half of the turns and go to LDS in the
+        // second: a wave's instructions wait for each other where many of a kind follow.
+        Mx4Operand w[2][kT], a = operand(buffer, 0, 0, ga, 0);
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(next[u], block + 4 * (U + u));
-        // kT products at a time, with the next rows on their way from LDS; in the second
-        // half of them what has been loaded goes there
-        Mx4Operand w[kT], a;
+        for (int t = 0; t < kT; ++t) w[0][t] = operand(buffer, 0, 1, gw + 2 * t, 0);
 #pragma unroll
         for (int turn = 0; turn < kTurns; ++turn) {
-            const int u = turn / (2 * kT), half = turn / kT % 2, i = turn % kT;
-            if (i == 0) {
-                a = operand(buffer, u, 0, ga, half);
-#pragma unroll
-                for (int t = 0; t < kT; ++t) w[t] = operand(buffer, u, 1, gw + 2 * t, half);
+            const int pass = turn / kT, i = turn % kT;   // a pass: two blocks
+            Mx4Operand after = a;
+            if (turn + 1 < kTurns) {
+                const int then = (turn + 1) / kT;
+                after = operand(buffer, then / 2, 0, ga + 2 * ((turn + 1) % kT), then % 2);
             }
-            const Mx4Operand after = operand(buffer, u, 0, ga + 2 * (i + 1 < kT ? i + 1 : i), half);
+            if (pass + 1 < 2 * U)
+                w[(pass + 1) % 2][i] =
+                    operand(buffer, (pass + 1) / 2, 1, gw + 2 * i, (pass + 1) % 2);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < kT; ++t) acc[i][t] = mx4_mfma32(w[t], a, acc[i][t]);
+            for (int t = 0; t < kT; ++t) acc[i][t] = mx4_mfma32(w[pass % 2][t], a, acc[i][t]);
 #pragma unroll
-            for (int x = 0; x < kPieces; ++x)
+            for (int x = 0; x < kPieces; ++x) {
+                if (x * (kTurns / 2) / kPieces == turn) load(block + 4 * U, x);
                 if (kTurns / 2 + x * (kTurns / 2) / kPieces == turn) store(buffer ^ 1, x);
+            }
             a = after;
             __builtin_amdgcn_sched_barrier(0);
         }
