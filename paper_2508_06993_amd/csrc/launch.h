@@ -249,6 +249,11 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
 hipError_t launch_mx4_linear(const octnca_rows &x, const octnca_mx4 &kept, const octnca_mx4 &w,
                              const float *bias, bool relu, const octnca_rows &out,
                              hipStream_t stream);
+// Products of narrow layers (mx4_narrow.hip), of the values x or (null) of a's codes.
+bool mx4_narrow_serves(int64_t cols, int64_t outs);
+hipError_t launch_mx4_narrow(const octnca_rows *x, const octnca_mx4 &a, const octnca_mx4 &w,
+                             const float *bias, bool relu, const octnca_rows &out,
+                             hipStream_t stream);
 size_t mx4_backward_bytes(int64_t rows, int64_t cols, int64_t outs);
 // grad_in, grad_weight, grad_bias may be null; rows may be 0.
 hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,

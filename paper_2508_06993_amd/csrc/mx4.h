@@ -111,4 +111,90 @@ __device__ __forceinline__ v16f32 mx4_mfma32(const Mx4Operand &a, const Mx4Opera
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 4, 4, 0, a.scale, 0, b.scale);
 }
 
+// x of lane K of each four lanes; of the lane's partner in them.
+template <int K> __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, K * 0x55, 15, 15, true);
+}
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 15, 15, true);
+    x = x > y ? x : y;
+    const uint32_t z = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 15, 15, true);
+    return x > z ? x : z;
+}
+
+// A unit is a block of a row group, 256 bytes of codes; a wave takes kUnits in a row.
+// Four lanes have a block of a row, eight columns each; sixteen the same row of all
+// units (with four blocks of a row 256 bytes of fp16 in a row), and a pass of the wave
+// four rows of each unit.
+constexpr int kUnits = 4, kPasses = 4;
+struct Place {
+    int64_t unit, row;   // row: of pass 0; of pass k 4 k more
+    int col;
+};
+__device__ __forceinline__ Place place_of(int64_t first, int blocks) {
+    const int lane = threadIdx.x & 63, unit = lane % 16 / 4;
+    int64_t group = first / blocks;
+    int block = (int)(first - group * blocks) + unit;
+    if (blocks >= kUnits) {
+        if (block >= blocks) block -= blocks, ++group;
+    } else {
+        group += block / blocks;
+        block %= blocks;
+    }
+    return Place{first + unit, group * kMxGroup + lane / 16, block * kMxBlock + lane % 4 * 8};
+}
+
+// The values of a wave's units.  NARROW: rows of fewer than eight columns.
+template <typename V, bool NARROW>
+__device__ __forceinline__ void load_units(const typename V::T *__restrict__ x, int64_t stride,
+                                           int cols, int64_t rows, const Place &p,
+                                           Eight<V> *raw) {
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+        const int64_t r = p.row + 4 * k;
+        const typename V::T *row = x + (r < rows ? r : rows - 1) * stride;
+        if (NARROW) {
+            raw[k].down = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                raw[k].v[e] = p.col + e < cols ? row[p.col + e] : (typename V::T)0.0f;
+        } else {
+            raw[k].load(row, p.col, cols);
+        }
+    }
+}
+
+// Codes of a lane's eight values and the scale byte of their block, for each pass.
+template <typename V>
+__device__ __forceinline__ void quantise_units(const Eight<V> *raw, uint32_t *codes,
+                                               uint32_t *scale) {
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+        float v[8];
+        raw[k].values(v);
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t mag = __float_as_uint(v[e]) & 0x7fffffffu;
+            top = top > mag ? top : mag;
+        }
+        scale[k] = mx4_scale(quad_max(top));
+        codes[k] = mx4_codes(v, mx4_inverse(scale[k]));
+    }
+}
+
+// Entry q of four for lane q of each four lanes.
+__device__ __forceinline__ uint32_t quad_pick(const uint32_t *x) {
+    const int q = threadIdx.x & 3;
+    return q < 2 ? q == 0 ? x[0] : x[1] : q == 2 ? x[2] : x[3];
+}
+
+// Orders a wave's own LDS accesses (a wave runs them in order; the compiler must
+// too).
+__device__ __forceinline__ void lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 }  // namespace octnca

@@ -13,38 +13,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int64_t kMaxGrid = int64_t(1) << 23;
 
-// x of lane K of each four lanes; of the lane's partner in them.
-template <int K> __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, K * 0x55, 15, 15, true);
-}
-__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
-    x = std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 15, 15, true));
-    return std::max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 15, 15, true));
-}
-
-// A unit is a block of a row group, 256 bytes of codes; a wave takes kUnits in a row.
-// Four lanes have a block of a row, eight columns each; sixteen the same row of all
-// units (with four blocks of a row 256 bytes of fp16 in a row), and a pass of the wave
-// four rows of each unit.
-constexpr int kUnits = 4, kPasses = 4;
-struct Place {
-    int64_t unit, row;   // row: of pass 0; of pass k 4 k more
-    int col;
-};
-__device__ __forceinline__ Place place_of(int64_t first, int blocks) {
-    const int lane = threadIdx.x & 63, unit = lane % 16 / 4;
-    int64_t group = first / blocks;
-    int block = (int)(first - group * blocks) + unit;
-    if (blocks >= kUnits) {
-        if (block >= blocks) block -= blocks, ++group;
-    } else {
-        group += block / blocks;
-        block %= blocks;
-    }
-    return Place{first + unit, group * kMxGroup + lane / 16, block * kMxBlock + lane % 4 * 8};
-}
-
-// NARROW: rows of fewer than eight columns.
 template <typename V, bool NARROW>
 __global__ __launch_bounds__(kThreads) void quantise(const typename V::T *__restrict__ x,
                                                      int64_t stride, int cols, Mx4View m,
@@ -55,36 +23,17 @@ __global__ __launch_bounds__(kThreads) void quantise(const typename V::T *__rest
          u += (int64_t)gridDim.x * (kThreads / 64) * kUnits) {
         const Place p = place_of(u, m.blocks);
         Eight<V> raw[kPasses];
+        load_units<V, NARROW>(x, stride, cols, m.rows, p, raw);
+        uint32_t c[kPasses], scale[kPasses];
+        quantise_units(raw, c, scale);
 #pragma unroll
-        for (int k = 0; k < kPasses; ++k) {
-            const typename V::T *row = x + std::min(p.row + 4 * k, m.rows - 1) * stride;
-            if (NARROW) {
-                raw[k].down = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    raw[k].v[e] = p.col + e < cols ? row[p.col + e] : (typename V::T)0.0f;
-            } else {
-                raw[k].load(row, p.col, cols);
-            }
-        }
-        uint32_t scale[kPasses];
-#pragma unroll
-        for (int k = 0; k < kPasses; ++k) {
-            float v[8];
-            raw[k].values(v);
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = std::max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-            scale[k] = mx4_scale(quad_max(top));
-            const uint32_t c = mx4_codes(v, mx4_inverse(scale[k]));
+        for (int k = 0; k < kPasses; ++k)
             if (p.row + 4 * k < m.rows)
-                ((uint32_t *)m.codes)[p.unit * 64 + (4 * k + lane / 16) * 4 + lane % 4] = c;
-        }
+                ((uint32_t *)m.codes)[p.unit * 64 + (4 * k + lane / 16) * 4 + lane % 4] = c[k];
         // lane q of a block's four stores the scale of pass q's row
         const int q = lane % 4;
-        const uint32_t s = q < 2 ? q == 0 ? scale[0] : scale[1] : q == 2 ? scale[2] : scale[3];
         if (p.row + 4 * q < m.rows)
-            m.scales[p.unit * kMxGroup + 4 * q + lane / 16] = (uint8_t)s;
+            m.scales[p.unit * kMxGroup + 4 * q + lane / 16] = (uint8_t)quad_pick(scale);
     }
 }
 
@@ -409,6 +358,8 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
 
 hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const float *bias,
                               bool relu, const octnca_rows &out, hipStream_t stream) {
+    if (mx4_narrow_serves(a.cols, w.rows))
+        return launch_mx4_narrow(nullptr, a, w, bias, relu, out, stream);
     return with_type(out.dtype, [&](auto type) {
         using V = decltype(type);
         const ProductArgs p{mx4_view(a), mx4_view(w), bias, relu, out.data, out.stride,
@@ -437,6 +388,8 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
 hipError_t launch_mx4_linear(const octnca_rows &x, const octnca_mx4 &kept, const octnca_mx4 &w,
                              const float *bias, bool relu, const octnca_rows &out,
                              hipStream_t stream) {
+    if (mx4_narrow_serves(kept.cols, w.rows))
+        return launch_mx4_narrow(&x, kept, w, bias, relu, out, stream);
     const hipError_t e = launch_mx4_quantise(x, kept, stream);
     return e == hipSuccess ? launch_mx4_product(kept, w, bias, relu, out, stream) : e;
 }

@@ -302,13 +302,6 @@ struct NarrowArgs {
     float *bias;          // [splits][outs] or null
 };
 
-// Orders a wave's own LDS accesses.
-__device__ __forceinline__ void wave_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 template <typename V, int NT, int KT, bool VEC>
 __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
     constexpr int kP = kParts<V>, kWaves = kThreads / 64;
@@ -420,7 +413,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
                 }
             }
         }
-        wave_fence();
+        lds_fence();
         if (b.sums || b.bias) {
             v8bf16 q[KT];
 #pragma unroll
@@ -436,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
                     acc_bias[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, g, acc_bias[n], 0, 0, 0);
                 }
         }
-        wave_fence();
+        lds_fence();
     }
     if (!b.sums && !b.bias) return;
     // the waves' sums, [wave][kN][kK], then their biases [wave][kN]
