@@ -164,23 +164,27 @@ __device__ __forceinline__ void load_units(const typename V::T *__restrict__ x, 
     }
 }
 
-// Codes of a lane's eight values and the scale byte of their block, for each pass.
+// Codes of a lane's eight values and the scale byte of their block, whose other
+// values four lanes in a row have.
+template <typename V>
+__device__ __forceinline__ void quantise_eight(const Eight<V> &raw, uint32_t &codes,
+                                               uint32_t &scale) {
+    float v[8];
+    raw.values(v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t mag = __float_as_uint(v[e]) & 0x7fffffffu;
+        top = top > mag ? top : mag;
+    }
+    scale = mx4_scale(quad_max(top));
+    codes = mx4_codes(v, mx4_inverse(scale));
+}
 template <typename V>
 __device__ __forceinline__ void quantise_units(const Eight<V> *raw, uint32_t *codes,
                                                uint32_t *scale) {
 #pragma unroll
-    for (int k = 0; k < kPasses; ++k) {
-        float v[8];
-        raw[k].values(v);
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t mag = __float_as_uint(v[e]) & 0x7fffffffu;
-            top = top > mag ? top : mag;
-        }
-        scale[k] = mx4_scale(quad_max(top));
-        codes[k] = mx4_codes(v, mx4_inverse(scale[k]));
-    }
+    for (int k = 0; k < kPasses; ++k) quantise_eight(raw[k], codes[k], scale[k]);
 }
 
 // Entry q of four for lane q of each four lanes.

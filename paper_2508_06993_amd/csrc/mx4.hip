@@ -1,6 +1,7 @@
 // Matrices in microscaled 4 bits: quantisation and product (formulas and layout
 // in octree_nca.h).
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "launch.h"
@@ -81,58 +82,125 @@ __global__ __launch_bounds__(kThreads) void dequantise(Mx4View m, typename V::T 
     }
 }
 
+// Values of few rows that every workgroup quantises for itself at most: as many as
+// that takes less time than a launch (4 us).
+constexpr int kFewValues = 16384;
+
 struct ProductArgs {
     Mx4View a, w;
     const float *bias;   // or null
     bool relu;
     void *out;
     int64_t stride;
-    bool vec;            // four outputs of a row from a multiple of four on can be stored at once
 };
 
-// Outputs n .. n + 3 of a row.
-template <typename V>
-__device__ __forceinline__ void put_outputs(const ProductArgs &p, int64_t row, int n, v4f32 acc) {
-    const int outs = (int)p.w.rows;
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[i] = acc[i] + (p.bias && n + i < outs ? p.bias[n + i] : 0.0f);
-        if (p.relu && y[i] < 0.0f) y[i] = 0.0f;
-    }
-    typename V::T *to = (typename V::T *)p.out + row * p.stride + n;
-    if (p.vec && n + 4 <= outs) {
-        V::put4(to, y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < outs) V::put(to + i, y[i]);
-    }
-}
-
-// A wave takes a row group and kTiles groups of outputs, straight from memory.
-constexpr int kTiles = 4;
-template <typename V>
-__global__ __launch_bounds__(kThreads) void product(ProductArgs p) {
+// Few rows.  A workgroup takes 16 outputs times 16 G rows, its waves a part of the
+// columns each: what there is to read, the weights, is on its way at once.  The waves'
+// sums are added in order.  X: type of the values that are quantised on the way (one
+// row group, few values: every workgroup does it for itself), or int: codes.
+constexpr int kAhead = 4;   // steps of four blocks that are loaded together
+template <typename V, typename X, int G, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_rows(ProductArgs p, const void *x,
+                                                       int64_t x_stride, int cols) {
+    constexpr bool kValues = !std::is_same<X, int>::value;
+    __shared__ float sums[WAVES][G][256];
+    __shared__ Words4 codes[kValues ? kFewValues / 32 : 1];   // [block][row]
+    __shared__ uint8_t scales[kValues ? kFewValues / 32 : 1];
     const int lane = threadIdx.x & 63;
-    const int64_t group = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    const int64_t groups = (p.a.rows + kMxGroup - 1) / kMxGroup;
-    const int w_groups = (int)((p.w.rows + kMxGroup - 1) / kMxGroup);
-    const int tile = blockIdx.y * kTiles;
-    if (group >= groups) return;
-    v4f32 acc[kTiles] = {};
-    for (int k = 0; k < p.a.blocks; k += 4) {
-        const Mx4Operand b = mx4_operand(p.a, group, k);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int blocks = p.a.blocks, rows = (int)p.a.rows;
+    const int64_t group0 = (int64_t)blockIdx.y * G, last = (p.a.rows + kMxGroup - 1) / kMxGroup - 1;
+    const int steps = (blocks + 3) / 4, each = (steps + WAVES - 1) / WAVES;
+    const int begin = wave * each, end = std::min(steps, begin + each);
+    const Words4 *w_codes = (const Words4 *)p.w.codes + (int64_t)blockIdx.x * blocks * kMxGroup;
+    const uint8_t *w_scales = p.w.scales + (int64_t)blockIdx.x * blocks * kMxGroup;
+
+    Mx4Operand w[kAhead];
+    const auto load_w = [&](int step) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-            acc[t] = mx4_mfma(mx4_operand(p.w, std::min(tile + t, w_groups - 1), k), b, acc[t]);
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = std::min((step + k) * 64 + lane, blocks * kMxGroup - 1);
+            w[k] = Mx4Operand{w_codes[at], w_scales[at]};
+        }
+    };
+    load_w(std::min(begin, steps - 1));
+    if constexpr (kValues) {
+        // four lanes a block, eight values each
+        const int parts = blocks * 4;
+        for (int e = threadIdx.x; e < (rows * parts + 63) / 64 * 64; e += 64 * WAVES) {
+            const int row = std::min(e / parts, rows - 1), col = (e - e / parts * parts) * 8;
+            const auto from = (const typename X::T *)x + row * x_stride;
+            Eight<X> raw;
+            if (cols < 8) {
+                raw.down = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    raw.v[k] = col + k < cols ? from[col + k] : (typename X::T)0.0f;
+            } else {
+                raw.load(from, col, cols);
+            }
+            uint32_t c, s;
+            quantise_eight(raw, c, s);
+            if (e < rows * parts) {
+                const int at = col / kMxBlock * rows + row;
+                ((uint32_t *)codes)[at * 4 + col % kMxBlock / 8] = c;
+                if (col % kMxBlock == 0) scales[at] = (uint8_t)s;
+                if (blockIdx.x == 0) {
+                    const int kept = col / kMxBlock * kMxGroup + row;
+                    ((uint32_t *)p.a.codes)[kept * 4 + col % kMxBlock / 8] = c;
+                    if (col % kMxBlock == 0) p.a.scales[kept] = (uint8_t)s;
+                }
+            }
+        }
+        __syncthreads();
     }
-    const int64_t row = group * kMxGroup + lane % kMxGroup;
-    if (row >= p.a.rows) return;
+    v4f32 acc[G] = {};
+    for (int step = begin; step < end; step += kAhead) {
+        Mx4Operand a[kAhead][G];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-        if (tile + t < w_groups)
-            put_outputs<V>(p, row, (tile + t) * kMxGroup + lane / kMxGroup * 4, acc[t]);
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int block = std::min((step + k) * 4 + lane / 16, blocks - 1);
+                if constexpr (kValues) {
+                    const int at = block * rows + std::min(lane % 16, rows - 1);
+                    a[k][g] = Mx4Operand{codes[at], scales[at]};
+                } else {
+                    const int64_t at = (std::min(group0 + g, last) * blocks + block) * kMxGroup + lane % 16;
+                    a[k][g] = Mx4Operand{((const Words4 *)p.a.codes)[at], p.a.scales[at]};
+                }
+            }
+        Mx4Operand now[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const bool in = step + k < end && (step + k) * 4 + lane / 16 < blocks;
+            now[k] = Mx4Operand{w[k].codes & (in ? ~0u : 0u), in ? w[k].scale : 127u};
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                if (!in) a[k][g].scale = 127;
+        }
+        load_w(std::min(step + kAhead, steps - 1));
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g) acc[g] = mx4_mfma(now[k], a[k][g], acc[g]);
+    }
+    // [output][row] of a row group
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[wave][g][(lane / 16 * 4 + i) * 16 + lane % 16] = acc[g][i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < G * 256; e += 64 * WAVES) {
+        const int g = e / 256, r = e % 256 / 16, n = e % 16;
+        const int64_t row = (group0 + g) * kMxGroup + r, out = (int64_t)blockIdx.x * kMxGroup + n;
+        if (row >= p.a.rows || out >= p.w.rows) continue;
+        float y = sums[0][g][n * 16 + r];
+        for (int v = 1; v < WAVES; ++v) y += sums[v][g][n * 16 + r];
+        if (p.bias) y += p.bias[out];
+        if (p.relu && y < 0.0f) y = 0.0f;
+        V::put((typename V::T *)p.out + row * p.stride + out, y);
+    }
 }
 
 // Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
@@ -356,32 +424,51 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
     });
 }
 
+// Which kernel serves a product that is not narrow.  Tiles of 256 x 256 where they
+// fill the card, tiles of 128 x 128 likewise, else a few rows at a time with the
+// columns split.
+namespace {
+
+template <typename V, typename X, int G>
+hipError_t run_few(const ProductArgs &p, const octnca_rows *x, int cols, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.w.rows + kMxGroup - 1) / kMxGroup),
+                    (unsigned)((p.a.rows + kMxGroup * G - 1) / (kMxGroup * G)));
+    const void *from = x ? x->data : nullptr;
+    const int64_t stride = x ? x->stride : 0;
+    // sixteen waves where there are few workgroups
+    if ((int64_t)grid.x * grid.y <= 128 && p.a.blocks > 16)
+        few_rows<V, X, G, 16><<<grid, 64 * 16, 0, stream>>>(p, from, stride, cols);
+    else
+        few_rows<V, X, G, 4><<<grid, 64 * 4, 0, stream>>>(p, from, stride, cols);
+    return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const float *bias,
                               bool relu, const octnca_rows &out, hipStream_t stream) {
     if (mx4_narrow_serves(a.cols, w.rows))
         return launch_mx4_narrow(nullptr, a, w, bias, relu, out, stream);
     return with_type(out.dtype, [&](auto type) {
         using V = decltype(type);
-        const ProductArgs p{mx4_view(a), mx4_view(w), bias, relu, out.data, out.stride,
-                            rows_aligned(out, 4 * V::kBytes)};
-        const auto tiles_of = [&](int side) {
+        const ProductArgs p{mx4_view(a), mx4_view(w), bias, relu, out.data, out.stride};
+        const auto tiles = [&](int64_t side) {
             return std::make_pair((a.rows + side - 1) / side, (w.rows + side - 1) / side);
         };
-        const auto large = tiles_of(256), small = tiles_of(128);
+        const auto large = tiles(256), small = tiles(128);
         if (large.first * large.second >= 192) {
             product_tiles<V, 8, 2><<<(unsigned)(large.first * large.second), kThreads, 0, stream>>>(
                 p, (int)large.first, (int)large.second);
             return hipGetLastError();
         }
-        if (small.first * small.second >= 128) {
+        if (a.rows > 64 && small.first * small.second >= 128) {
             product_tiles<V, 4, 2><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
                 p, (int)small.first, (int)small.second);
             return hipGetLastError();
         }
-        const int64_t groups = (a.rows + kMxGroup - 1) / kMxGroup;
-        const int64_t tiles = (w.rows + kMxGroup * kTiles - 1) / (kMxGroup * kTiles);
-        product<V><<<dim3((unsigned)((groups + 3) / 4), (unsigned)tiles), kThreads, 0, stream>>>(p);
-        return hipGetLastError();
+        return a.rows <= 16   ? run_few<V, int, 1>(p, nullptr, (int)a.cols, stream)
+               : a.rows <= 32 ? run_few<V, int, 2>(p, nullptr, (int)a.cols, stream)
+                              : run_few<V, int, 4>(p, nullptr, (int)a.cols, stream);
     });
 }
 
@@ -390,6 +477,13 @@ hipError_t launch_mx4_linear(const octnca_rows &x, const octnca_mx4 &kept, const
                              hipStream_t stream) {
     if (mx4_narrow_serves(kept.cols, w.rows))
         return launch_mx4_narrow(&x, kept, w, bias, relu, out, stream);
+    if (kept.rows <= kMxGroup && kept.rows * mx4_blocks(kept.cols) * kMxBlock <= kFewValues)
+        return with_type(out.dtype, [&](auto type) {
+            return with_type(x.dtype, [&](auto x_type) {
+                const ProductArgs p{mx4_view(kept), mx4_view(w), bias, relu, out.data, out.stride};
+                return run_few<decltype(type), decltype(x_type), 1>(p, &x, (int)kept.cols, stream);
+            });
+        });
     const hipError_t e = launch_mx4_quantise(x, kept, stream);
     return e == hipSuccess ? launch_mx4_product(kept, w, bias, relu, out, stream) : e;
 }
