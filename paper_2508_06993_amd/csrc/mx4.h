@@ -38,12 +38,12 @@ __device__ __forceinline__ float mx4_scale_value(uint32_t scale) {
 // Codes of eight values times `inverse` (exact: a power of two), the first
 // lowest.  A block of NaN has codes 0.
 __device__ __forceinline__ uint32_t mx4_codes(const float *x, float inverse) {
-    if (inverse == 0.0f) return 0;
     uint32_t c = 0;
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * inverse, x[1] * inverse, 1.0f, 0);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * inverse, x[3] * inverse, 1.0f, 1);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inverse, x[5] * inverse, 1.0f, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inverse, x[7] * inverse, 1.0f, 3);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inverse, x[7] * inverse, 1.0f, 3);
+    return inverse == 0.0f ? 0 : c;
 }
 
 // The values of eight codes (without their scale).
@@ -187,10 +187,12 @@ __device__ __forceinline__ void quantise_units(const Eight<V> *raw, uint32_t *co
     for (int k = 0; k < kPasses; ++k) quantise_eight(raw[k], codes[k], scale[k]);
 }
 
-// Entry q of four for lane q of each four lanes.
+// Entry q of four for lane q of each four lanes (selects of values: an index would
+// put the array into memory).
 __device__ __forceinline__ uint32_t quad_pick(const uint32_t *x) {
-    const int q = threadIdx.x & 3;
-    return q < 2 ? q == 0 ? x[0] : x[1] : q == 2 ? x[2] : x[3];
+    const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
+    const uint32_t even = threadIdx.x & 2 ? x2 : x0, odd = threadIdx.x & 2 ? x3 : x1;
+    return threadIdx.x & 1 ? odd : even;
 }
 
 // Orders a wave's own LDS accesses (a wave runs them in order; the compiler must
