@@ -52,7 +52,6 @@ struct BackwardArgs {
     Mx4View q;            // the weights (grad_in) or the inputs (grad_weight)
     void *out;            // grad_in, or grad_weight's sums [splits][outs][cols] or null
     int64_t out_stride;
-    bool out_vec;         // out's rows start at multiples of four values
     float *bias;          // sums [splits][outs], or null
     int64_t per_split;    // rows of a split (a multiple of kStep)
 };
@@ -65,6 +64,21 @@ __device__ __forceinline__ v8bf16 read_columns(const uint16_t *tile, int col) {
     typedef __attribute__((address_space(3))) v4i16 *Lds;
     const int lane = threadIdx.x & 63;
     const uint16_t *at = tile + (lane / 16 * 8 + lane % 16 / 4) * PITCH + col + lane % 4 * 4;
+    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+    const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * PITCH));
+    return __builtin_bit_cast(v8bf16, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// The same for 32 columns and 16 rows from `row` on (an operand of the 32 x 32
+// instruction): lane l gets column l % 32, rows 8 (l / 32) .. + 7.  SWAP: the second
+// and third four of each sixteen columns change places.
+template <int PITCH, bool SWAP>
+__device__ __forceinline__ v8bf16 read_columns32(const uint16_t *tile, int row, int col) {
+    typedef __attribute__((address_space(3))) v4i16 *Lds;
+    const int lane = threadIdx.x & 63;
+    const int four = SWAP ? (lane & 1) * 2 + (lane >> 1 & 1) : lane & 3;
+    const uint16_t *at = tile + (row + lane / 32 * 8 + lane % 16 / 4) * PITCH + col +
+                         lane % 32 / 16 * 16 + four * 4;
     const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
     const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * PITCH));
     return __builtin_bit_cast(v8bf16, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -137,147 +151,165 @@ __device__ __forceinline__ Words4 code_values(uint32_t codes, uint32_t scale) {
 
 // out[i][j] = sum over c of P[i][c] Q[c][j], Q the values of a matrix in 4 bits.
 // WEIGHT: i an output, c a row of G, j a column of the inputs (P = G^T); else i a
-// row of G, c an output, j a column of the weights.  A workgroup takes 32 I rows and
-// 32 J columns, four waves with a quarter each.  The next step's values are on
-// their way into registers while this one's are multiplied.
-template <typename V, bool WEIGHT, int I, int J, bool VEC>
+// row of G, c an output, j a column of the weights.  A workgroup takes 64 I rows and
+// 64 I columns, four waves with a quarter each, U steps at a time.  The next ones are
+// loaded during the first half of the products and go to LDS, as bf16 values, during
+// the second.
+template <typename V, bool WEIGHT, int I, int U, bool VEC>
 __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     constexpr int kP = kParts<V>;
-    constexpr int kBi = 32 * I, kBj = 32 * J;
-    constexpr int kPitchP = WEIGHT ? kBi + kPad : kStep + 8;
-    constexpr int kRowsP = WEIGHT ? kStep : kBi;
-    constexpr int kPitchQ = kBj + kPad;
-    constexpr int kLoadsP = kBi / 64, kLoadsQ = kBj / 64;
-    static_assert(kBi % 64 == 0 && kBj % 64 == 0, "whole loads");
-    __shared__ __align__(16) uint16_t ps[2][kP][kRowsP * kPitchP];
-    __shared__ __align__(16) uint16_t qs[2][kStep * kPitchQ];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i0 = (WEIGHT ? (int64_t)blockIdx.y : (int64_t)blockIdx.x) * kBi;
-    const int j0 = (WEIGHT ? blockIdx.x : blockIdx.y) * kBj;
+    constexpr int kSide = 64 * I;
+    constexpr int kPitchP = WEIGHT ? kSide + kPad : kStep + 8;
+    constexpr int kRowsP = WEIGHT ? kStep : kSide;
+    constexpr int kPitchQ = kSide + kPad;
+    constexpr int kLoads = kSide / 64;   // of a thread and side
+    // a lane's results of four columns, or of eight for 16-bit types
+    using O = std::conditional_t<WEIGHT, Values<OCTNCA_F32>, V>;
+    constexpr int kRun = 16 / O::kBytes;
+    __shared__ __align__(16) uint16_t ps[2][U][kP][kRowsP * kPitchP];
+    __shared__ __align__(16) uint16_t qs[2][U][kStep * kPitchQ];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t i0 = (WEIGHT ? (int64_t)blockIdx.y : (int64_t)blockIdx.x) * kSide;
+    const int j0 = (WEIGHT ? blockIdx.x : blockIdx.y) * kSide;
     const int64_t i_end = WEIGHT ? b.outs : b.rows;
     const int64_t c_begin = WEIGHT ? (int64_t)blockIdx.z * b.per_split : 0;
     const int64_t c_end = WEIGHT ? std::min(b.rows, c_begin + b.per_split) : b.outs;
     const bool sum_bias = WEIGHT && b.bias != nullptr && j0 == 0;
     const auto grad = (const typename V::T *)b.grad;
 
-    Raw8<V> p[kLoadsP];
-    uint32_t codes[kLoadsQ], scales[kLoadsQ];
-    bool codes_in[kLoadsQ];
+    Raw8<V> p[U][kLoads];
+    uint32_t codes[U][kLoads], scales[U][kLoads];
+    bool codes_in[U][kLoads];
     // where a thread's part k of P lies: row and first column of the tile
     const auto p_row = [&](int k) {
-        return WEIGHT ? (threadIdx.x + k * kThreads) / (kBi / 8) : threadIdx.x / 4 + k * 64;
+        return WEIGHT ? (threadIdx.x + k * kThreads) / (kSide / 8) : threadIdx.x / 4 + k * 64;
     };
     const auto p_col = [&](int k) {
-        return WEIGHT ? (threadIdx.x + k * kThreads) % (kBi / 8) * 8 : threadIdx.x % 4 * 8;
+        return WEIGHT ? (threadIdx.x + k * kThreads) % (kSide / 8) * 8 : threadIdx.x % 4 * 8;
     };
-    const auto load = [&](int64_t c0) {
-#pragma unroll
-        for (int k = 0; k < kLoadsP; ++k) {
+    // Piece x of what is loaded: a part of P, or a block of a row group of Q
+    constexpr int kPieces = 2 * U * kLoads;
+    const auto load = [&](int64_t from, int x) {
+        const int u = x / (2 * kLoads), k = x % kLoads;
+        const int64_t c0 = from + u * kStep;
+        if (x % (2 * kLoads) < kLoads) {
             const int64_t row = (WEIGHT ? c0 : i0) + p_row(k), rows = WEIGHT ? c_end : i_end;
-            p[k].template load<VEC>(grad + std::min(row, rows - 1) * b.stride,
-                                    (WEIGHT ? i0 : c0) + p_col(k), WEIGHT ? i_end : c_end,
-                                    row < rows);
-        }
-        // a wave takes a block of a row group: 256 bytes
-#pragma unroll
-        for (int k = 0; k < kLoadsQ; ++k) {
+            p[u][k].template load<VEC>(grad + std::min(row, rows - 1) * b.stride,
+                                       (WEIGHT ? i0 : c0) + p_col(k), WEIGHT ? i_end : c_end,
+                                       row < rows);
+        } else {
             const int unit = k * 4 + wave, block = j0 / kMxBlock + unit / 2;
             const int64_t c = c0 + unit % 2 * kMxGroup + lane / 4;
-            codes_in[k] = c < c_end && block < b.q.blocks;
+            codes_in[u][k] = c < c_end && block < b.q.blocks;
             const int64_t row = std::min(c, c_end - 1);
             const int64_t at = (row / kMxGroup * b.q.blocks + std::min(block, b.q.blocks - 1)) *
                                    kMxGroup + row % kMxGroup;
-            codes[k] = ((const uint32_t *)b.q.codes)[at * 4 + lane % 4];
-            scales[k] = b.q.scales[at];
+            codes[u][k] = ((const uint32_t *)b.q.codes)[at * 4 + lane % 4];
+            scales[u][k] = b.q.scales[at];
         }
     };
     float bias[8] = {};
-    const auto store = [&](int buffer) {
-#pragma unroll
-        for (int k = 0; k < kLoadsP; ++k) {
+    const auto store = [&](int buffer, int x) {
+        const int u = x / (2 * kLoads), k = x % kLoads;
+        if (x % (2 * kLoads) < kLoads) {
             Words4 part[kP];
-            p[k].template parts<kP>(part);
+            p[u][k].template parts<kP>(part);
 #pragma unroll
             for (int q = 0; q < kP; ++q)
-                *(Words4 *)&ps[buffer][q][p_row(k) * kPitchP + p_col(k)] = part[q];
+                *(Words4 *)&ps[buffer][u][q][p_row(k) * kPitchP + p_col(k)] = part[q];
             if (sum_bias) {   // a thread's parts are of the same eight columns
-                float x[8];
-                p[k].values(x);
+                float y[8];
+                p[u][k].values(y);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) bias[e] += x[e];
+                for (int e = 0; e < 8; ++e) bias[e] += y[e];
             }
-        }
-#pragma unroll
-        for (int k = 0; k < kLoadsQ; ++k) {
+        } else {
             const int unit = k * 4 + wave;
-            *(Words4 *)&qs[buffer][(unit % 2 * kMxGroup + lane / 4) * kPitchQ +
-                                   unit / 2 * kMxBlock + lane % 4 * 8] =
-                code_values(codes_in[k] ? codes[k] : 0, codes_in[k] ? scales[k] : 127);
+            *(Words4 *)&qs[buffer][u][(unit % 2 * kMxGroup + lane / 4) * kPitchQ +
+                                      unit / 2 * kMxBlock + lane % 4 * 8] =
+                code_values(codes_in[u][k] ? codes[u][k] : 0, codes_in[u][k] ? scales[u][k] : 127);
         }
     };
 
-    v4f32 acc[I][J] = {};
-    const int wi = wave % 2 * (16 * I), wj = wave / 2 * (16 * J);
+    const int wi = wave % 2 * (32 * I), wj = wave / 2 * (32 * I);
+    // A turn: part turn % kP of 32 rows, 16 of the summed index; a pass: I * kP turns.
+    constexpr int kTurns = 2 * U * I * kP;
+    const auto operand = [&](int buffer, int turn) {
+        const int pass = turn / (I * kP), row = wi + turn / kP % I * 32;
+        const uint16_t *tile = ps[buffer][pass / 2][turn % kP];
+        return WEIGHT ? read_columns32<kPitchP, false>(tile, pass % 2 * 16, row)
+                      : *(const v8bf16 *)&tile[(row + lane % 32) * kPitchP + pass % 2 * 16 +
+                                               lane / 32 * 8];
+    };
+    const auto column_operand = [&](int buffer, int pass, int t) {
+        return read_columns32<kPitchQ, kRun == 8>(qs[buffer][pass / 2], pass % 2 * 16, wj + t * 32);
+    };
+    v16f32 acc[I][I] = {};
     if (c_begin < c_end) {
-        load(c_begin);
-        store(0);
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) load(c_begin, x);
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) store(0, x);
     }
     int buffer = 0;
-    for (int64_t c0 = c_begin; c0 < c_end; c0 += kStep, buffer ^= 1) {
+    for (int64_t c0 = c_begin; c0 < c_end; c0 += U * kStep, buffer ^= 1) {
         __syncthreads();
-        load(c0 + kStep);   // past the end: zeros, used by no one
-        const auto operand = [&](int u) {   // part u % kP of rows u / kP
-            const uint16_t *tile = ps[buffer][u % kP];
-            const int row = wi + u / kP * 16;
-            return WEIGHT ? read_columns<kPitchP>(tile, row)
-                          : *(const v8bf16 *)&tile[(row + lane % 16) * kPitchP + lane / 16 * 8];
-        };
-        v8bf16 q[J], g = operand(0);
+        v8bf16 q[2][I], g = operand(buffer, 0);
 #pragma unroll
-        for (int t = 0; t < J; ++t) q[t] = read_columns<kPitchQ>(qs[buffer], wj + t * 16);
+        for (int t = 0; t < I; ++t) q[0][t] = column_operand(buffer, 0, t);
 #pragma unroll
-        for (int u = 0; u < I * kP; ++u) {
-            const v8bf16 after = operand(u + 1 < I * kP ? u + 1 : u);
-            __builtin_amdgcn_sched_barrier(0);   // on its way during these
+        for (int turn = 0; turn < kTurns; ++turn) {
+            const int pass = turn / (I * kP);
+            const v8bf16 after = turn + 1 < kTurns ? operand(buffer, turn + 1) : g;
+            if (pass + 1 < 2 * U && turn % kP == 0)
+                q[(pass + 1) % 2][turn / kP % I] =
+                    column_operand(buffer, pass + 1, turn / kP % I);
+            __builtin_amdgcn_sched_barrier(0);   // on their way during these
 #pragma unroll
-            for (int t = 0; t < J; ++t)
-                acc[u / kP][t] =
-                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t], g, acc[u / kP][t], 0, 0, 0);
+            for (int t = 0; t < I; ++t)
+                acc[turn / kP % I][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    q[pass % 2][t], g, acc[turn / kP % I][t], 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x) {   // past the end: zeros, used by no one
+                if (x * (kTurns / 2) / kPieces == turn) load(c0 + U * kStep, x);
+                if (kTurns / 2 + x * (kTurns / 2) / kPieces == turn) store(buffer ^ 1, x);
+            }
             g = after;
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        store(buffer ^ 1);
     }
-    // a lane has four columns j of row i
-    using O = std::conditional_t<WEIGHT, Values<OCTNCA_F32>, V>;
+    // kRun columns of row lane % 32 of each tile in a row, the next ones 2 kRun on
     auto out = (typename O::T *)b.out;
     if (WEIGHT && out) out += (int64_t)blockIdx.z * b.outs * b.cols;
 #pragma unroll
-    for (int s = 0; s < I; ++s)
+    for (int s = 0; s < I; ++s) {
+        const int64_t i = i0 + wi + s * 32 + lane % 32;
+        if (i >= i_end || (WEIGHT && out == nullptr)) continue;
 #pragma unroll
-        for (int t = 0; t < J; ++t) {
-            const int64_t i = i0 + wi + s * 16 + lane % 16;
-            const int j = j0 + wj + t * 16 + lane / 16 * 4;
-            if (i >= i_end || (WEIGHT && out == nullptr)) continue;
-            const float y[4] = {acc[s][t][0], acc[s][t][1], acc[s][t][2], acc[s][t][3]};
-            auto to = out + i * b.out_stride + j;
-            if (b.out_vec && j + 4 <= b.cols) {
-                O::put4(to, y);
-            } else {
+        for (int t = 0; t < I; ++t)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (j + k < b.cols) O::put(to + k, y[k]);
+            for (int r = 0; r < 16 / kRun; ++r) {
+                float y[kRun];
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) y[k] = acc[s][t][r * kRun + k];
+                const int j = j0 + wj + t * 32 + r * 2 * kRun + lane / 32 * kRun;
+                if (j >= b.cols) continue;
+                if constexpr (kRun == 8)
+                    store8<O>(out + i * b.out_stride + j, y, b.cols - j);
+                else
+                    store4<O>(out + i * b.out_stride + j, y, b.cols - j);
             }
-        }
+    }
     if (sum_bias) {
-        // kBi / 8 threads hold the columns, the others more rows of them
-        constexpr int kSets = kThreads / (kBi / 8);
-        __shared__ float sums[kSets][kBi];
+        // kSide / 8 threads hold the columns, the others more rows of them
+        constexpr int kSets = kThreads / (kSide / 8);
+        __shared__ float sums[kSets][kSide];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            sums[threadIdx.x / (kBi / 8)][threadIdx.x % (kBi / 8) * 8 + e] = bias[e];
+            sums[threadIdx.x / (kSide / 8)][threadIdx.x % (kSide / 8) * 8 + e] = bias[e];
         __syncthreads();
-        for (int i = threadIdx.x; i < kBi; i += kThreads) {
+        for (int i = threadIdx.x; i < kSide; i += kThreads) {
             float x = 0.0f;
             for (int k = 0; k < kSets; ++k) x += sums[k][i];
             if (i0 + i < i_end) b.bias[(int64_t)blockIdx.z * b.outs + i0 + i] = x;
@@ -487,11 +519,11 @@ __global__ __launch_bounds__(64 * kJoin) void join(JoinArgs a) {
     }
 }
 
-constexpr int kLarge = 8, kSmall = 4;   // I and J of the two tile sizes
+constexpr int kLarge = 4, kSmall = 2;   // I of the two tile sizes
 
 // Whether a result of i x j values is cut into large tiles: where they fill the card.
 bool large_tiles(int64_t i, int64_t j) {
-    constexpr int64_t kSide = 32 * kLarge;
+    constexpr int64_t kSide = 64 * kLarge;
     return j > kSide / 2 && ((i + kSide - 1) / kSide) * ((j + kSide - 1) / kSide) >= 192;
 }
 
@@ -511,7 +543,7 @@ int splits_of(int64_t rows, int64_t cols, int64_t outs) {
     const int64_t most = std::max<int64_t>(1, (rows + 127) / 128);
     if (narrow_of(cols, outs).nt) return (int)std::min<int64_t>(512, most);
     const bool large = large_tiles(outs, cols);
-    const int64_t side = 32 * (large ? kLarge : kSmall);
+    const int64_t side = 64 * (large ? kLarge : kSmall);
     const int64_t tiles = ((cols + side - 1) / side) * ((outs + side - 1) / side);
     return (int)std::min(((large ? 256 : 512) + tiles - 1) / tiles, (most + 1) / 2);
 }
@@ -520,15 +552,17 @@ size_t sums_bytes(int64_t splits, int64_t cols, int64_t outs) {
     return (size_t)splits * (size_t)outs * (size_t)(cols + 1) * 4;
 }
 
-template <typename V, bool WEIGHT, int S>
+template <typename V, bool WEIGHT, int I>
 void run_tiles(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
-    const auto tiles = [](int64_t n) { return (unsigned)((n + 32 * S - 1) / (32 * S)); };
+    // two steps at a time where LDS has room for them
+    constexpr int U = kParts<V> == 1 ? 2 : 1;
+    const auto tiles = [](int64_t n) { return (unsigned)((n + 64 * I - 1) / (64 * I)); };
     const unsigned i = tiles(WEIGHT ? b.outs : b.rows), j = products ? tiles(b.cols) : 1;
     const dim3 grid = WEIGHT ? dim3(j, i, splits) : dim3(i, j, 1);
     if (b.vec)
-        backward<V, WEIGHT, S, S, true><<<grid, kThreads, 0, stream>>>(b);
+        backward<V, WEIGHT, I, U, true><<<grid, kThreads, 0, stream>>>(b);
     else
-        backward<V, WEIGHT, S, S, false><<<grid, kThreads, 0, stream>>>(b);
+        backward<V, WEIGHT, I, U, false><<<grid, kThreads, 0, stream>>>(b);
 }
 
 template <typename V, bool WEIGHT>
@@ -605,14 +639,12 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
                 b.q = mx4_view(w);
                 b.out = grad_in->data;
                 b.out_stride = grad_in->stride;
-                b.out_vec = aligned(*grad_in, 4 * V::kBytes);
                 run<V, false>(b, 1, true, stream);
             }
             if (grad_weight || grad_bias) {
                 b.q = mx4_view(a);
                 b.out = grad_weight ? sums : nullptr;
                 b.out_stride = cols;
-                b.out_vec = cols % 4 == 0 && (uintptr_t)sums % 16 == 0;
                 b.bias = grad_bias ? bias_sums : nullptr;
                 b.per_split = ((rows + splits - 1) / splits + kStep - 1) / kStep * kStep;
                 run<V, true>(b, splits, grad_weight != nullptr, stream);
