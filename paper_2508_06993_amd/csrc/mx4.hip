@@ -203,6 +203,20 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows(ProductArgs p, const void
     }
 }
 
+// Tile of a workgroup among row_tiles x col_tiles.  Workgroups go round the eight dies,
+// each with its own L2: a die takes tiles in a row, which run down eight row tiles
+// before they go to the next columns.
+struct Tile {
+    int row, col;
+};
+__device__ __forceinline__ Tile die_tile(int id, int row_tiles, int col_tiles) {
+    const int each = row_tiles * col_tiles / 8;
+    if (id < each * 8) id = id % 8 * each + id / 8;
+    const int band = id / (8 * col_tiles), left = row_tiles - band * 8, deep = left < 8 ? left : 8;
+    const int in_band = id - band * 8 * col_tiles;
+    return Tile{band * 8 + in_band % deep, in_band / deep};
+}
+
 // Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
 // them with its sums in registers.  128 columns at a time (four blocks) go through
 // LDS, loaded two steps ahead of their use: one step's products take about half of
@@ -218,15 +232,8 @@ __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row
     __shared__ uint32_t scales[2][U][2][kGroups][16];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go round the eight dies, each with its own L2: a die takes tiles in
-    // a row, which run down eight row tiles before they go to the next outputs.
-    int tile = blockIdx.x;
-    const int each = (int)gridDim.x / 8;
-    if (tile < each * 8) tile = tile % 8 * each + tile / 8;
-    const int band = tile / (8 * out_tiles), deep = std::min(8, row_tiles - band * 8);
-    const int in_band = tile - band * 8 * out_tiles;
-    const int64_t group0[2] = {(int64_t)(band * 8 + in_band % deep) * kGroups,
-                               (int64_t)(in_band / deep) * kGroups};
+    const Tile tile = die_tile(blockIdx.x, row_tiles, out_tiles);
+    const int64_t group0[2] = {(int64_t)tile.row * kGroups, (int64_t)tile.col * kGroups};
     const Mx4View side[2] = {p.a, p.w};
     const int blocks = p.a.blocks;
 

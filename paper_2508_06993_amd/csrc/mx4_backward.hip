@@ -54,6 +54,7 @@ struct BackwardArgs {
     int64_t out_stride;
     float *bias;          // sums [splits][outs], or null
     int64_t per_split;    // rows of a split (a multiple of kStep)
+    int i_tiles, j_tiles; // of the result
 };
 
 // A tile of bf16 values in LDS, the summed index along the rows: the operand of 16
@@ -170,10 +171,11 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     __shared__ __align__(16) uint16_t qs[2][U][kStep * kPitchQ];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t i0 = (WEIGHT ? (int64_t)blockIdx.y : (int64_t)blockIdx.x) * kSide;
-    const int j0 = (WEIGHT ? blockIdx.x : blockIdx.y) * kSide;
+    // workgroups next to each other share columns (grad_in), or rows
+    const int64_t i0 = (int64_t)(WEIGHT ? blockIdx.x / b.j_tiles : blockIdx.x % b.i_tiles) * kSide;
+    const int j0 = (int)(WEIGHT ? blockIdx.x % b.j_tiles : blockIdx.x / b.i_tiles) * kSide;
     const int64_t i_end = WEIGHT ? b.outs : b.rows;
-    const int64_t c_begin = WEIGHT ? (int64_t)blockIdx.z * b.per_split : 0;
+    const int64_t c_begin = WEIGHT ? (int64_t)blockIdx.y * b.per_split : 0;
     const int64_t c_end = WEIGHT ? std::min(b.rows, c_begin + b.per_split) : b.outs;
     const bool sum_bias = WEIGHT && b.bias != nullptr && j0 == 0;
     const auto grad = (const typename V::T *)b.grad;
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     }
     // kRun columns of row lane % 32 of each tile in a row, the next ones 2 kRun on
     auto out = (typename O::T *)b.out;
-    if (WEIGHT && out) out += (int64_t)blockIdx.z * b.outs * b.cols;
+    if (WEIGHT && out) out += (int64_t)blockIdx.y * b.outs * b.cols;
 #pragma unroll
     for (int s = 0; s < I; ++s) {
         const int64_t i = i0 + wi + s * 32 + lane % 32;
@@ -312,7 +314,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
         for (int i = threadIdx.x; i < kSide; i += kThreads) {
             float x = 0.0f;
             for (int k = 0; k < kSets; ++k) x += sums[k][i];
-            if (i0 + i < i_end) b.bias[(int64_t)blockIdx.z * b.outs + i0 + i] = x;
+            if (i0 + i < i_end) b.bias[(int64_t)blockIdx.y * b.outs + i0 + i] = x;
         }
     }
 }
@@ -493,7 +495,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
 
 // to[e] = sum of from[s][e] over the splits s, of two lists; a wave takes every
 // kJoin-th split of 64 elements, and the waves' sums are added in order.
-constexpr int kJoin = 8;
+constexpr int kJoin = 16;
 struct JoinArgs {
     const float *from[2];
     float *to[2];
@@ -509,7 +511,7 @@ __global__ __launch_bounds__(64 * kJoin) void join(JoinArgs a) {
     const float *from = a.from[which];
     double x = 0.0;
     if (e < n)
-#pragma unroll 4
+#pragma unroll 8
         for (int s = wave; s < a.splits; s += kJoin) x += from[s * n + e];
     sums[wave][lane] = x;
     __syncthreads();
@@ -553,12 +555,13 @@ size_t sums_bytes(int64_t splits, int64_t cols, int64_t outs) {
 }
 
 template <typename V, bool WEIGHT, int I>
-void run_tiles(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
+void run_tiles(BackwardArgs b, int splits, bool products, hipStream_t stream) {
     // two steps at a time where LDS has room for them
     constexpr int U = kParts<V> == 1 ? 2 : 1;
     const auto tiles = [](int64_t n) { return (unsigned)((n + 64 * I - 1) / (64 * I)); };
-    const unsigned i = tiles(WEIGHT ? b.outs : b.rows), j = products ? tiles(b.cols) : 1;
-    const dim3 grid = WEIGHT ? dim3(j, i, splits) : dim3(i, j, 1);
+    b.i_tiles = (int)tiles(WEIGHT ? b.outs : b.rows);
+    b.j_tiles = products ? (int)tiles(b.cols) : 1;
+    const dim3 grid((unsigned)(b.i_tiles * b.j_tiles), (unsigned)splits);
     if (b.vec)
         backward<V, WEIGHT, I, U, true><<<grid, kThreads, 0, stream>>>(b);
     else

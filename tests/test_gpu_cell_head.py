@@ -1,0 +1,207 @@
+"""Cell layers as they are used together: a head on an inference's final state,
+trained with dropout and AdamW; replayed graphs; other streams; several layers."""
+import numpy as np
+import pytest
+import torch
+
+import cells4
+import paper_2508_06993_amd as octnca
+from paper_2508_06993_amd.runtime import (CellLayer, Dropout, Inference, MX4Matrix, Parameters,
+                                          upload_weights)
+from synthetic import TINY_2D, make_image, make_weights
+
+pytestmark = pytest.mark.gpu
+
+CLASSES, HIDDEN = 19, 48
+
+
+class Head:
+    """16 channels -> 48 hidden units, ReLU and dropout -> 19 scores, for every cell."""
+
+    def __init__(self, cells, seed, rate=0.25):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        new = lambda *s: torch.randn(*s, generator=gen, device="cuda") * s[-1] ** -0.5
+        self.w = [new(HIDDEN, 16), new(CLASSES, HIDDEN)]
+        self.b = [torch.zeros(HIDDEN, device="cuda"), torch.zeros(CLASSES, device="cuda")]
+        self.layers = [CellLayer(w, b, rows=cells, train=True) for w, b in zip(self.w, self.b)]
+        self.step = torch.zeros(1, dtype=torch.int64, device="cuda")
+        self.drop = Dropout(rate, seed + 77, self.step)
+        full = lambda n: torch.zeros(cells, n, device="cuda")
+        self.pre, self.hidden, self.grad_hidden = full(HIDDEN), full(HIDDEN), full(HIDDEN)
+        self.scores, self.grad_scores, self.grad_state = full(CLASSES), full(CLASSES), full(16)
+        grads = [t for l in self.layers for t in (l.grad_weight, l.grad_bias)]
+        params = [t for pair in zip(self.w, self.b) for t in pair]
+        m, v = ([torch.zeros_like(p) for p in params] for _ in range(2))
+        self.parameters = Parameters(grads, params, m, v, step=self.step)
+
+    def forward(self, state, stream=None):
+        self.layers[0].forward(state, self.pre, stream=stream)
+        self.drop(self.pre, self.hidden, gate=self.pre, stream=stream)
+        self.layers[1].forward(self.hidden, self.scores, stream=stream)
+        return self.scores
+
+    def backward(self, target, stream=None):
+        torch.sub(self.scores, target, out=self.grad_scores)
+        self.layers[1].backward(self.grad_scores, self.grad_hidden, stream=stream)
+        self.drop(self.grad_hidden, self.grad_hidden, gate=self.pre, stream=stream)
+        self.layers[0].backward(self.grad_hidden, self.grad_state, stream=stream)
+
+    def train(self, state, target, stream=None):
+        self.forward(state, stream)
+        self.backward(target, stream)
+        self.parameters.adamw(1e-2, stream=stream)
+        for layer in self.layers:
+            layer.refresh(stream)
+
+
+def final_state():
+    model = octnca.Model(ndim=2, n_in=3)
+    run = Inference(model, TINY_2D.extent, TINY_2D.factors)
+    image = torch.from_numpy(np.ascontiguousarray(make_image(TINY_2D))).to("cuda", torch.float32)
+    state, _ = run(image, upload_weights(make_weights(TINY_2D)), TINY_2D.steps, 0.5, 0)
+    return state
+
+
+def values(m):
+    return m.dequantise(torch.empty(m.used, m.cols, device="cuda")).double().cpu()
+
+
+def test_head_on_a_state(gpu):
+    """Every tensor of one training step against 64 bits on the CPU, from the values
+    that 4 bits hold of its own inputs."""
+    state = final_state()
+    cells = state[..., 0].numel()
+    head = Head(cells, 3)
+    target = torch.randn(cells, CLASSES, device=gpu)
+    head.forward(state)
+    head.backward(target)
+    x, w0, w1 = values(head.layers[0].kept), values(head.layers[0].w), values(head.layers[1].w)
+    want = cells4.quantise(state.reshape(cells, 16)[:200].double().cpu().numpy())[0]
+    assert np.array_equal(x[:200].numpy(), want)
+
+    def close(got, want, mags, terms):
+        bound = (terms + 3) * 2.0 ** -23 * mags + 2.0 ** -24 * want.abs() + 2.0 ** -120
+        assert ((got.double().cpu() - want).abs() <= bound).all()
+    pre = x @ w0.t()
+    close(head.pre, pre, x.abs() @ w0.abs().t(), 16)
+    draws = cells4.draws(range(400), 80, 0)
+    kept = torch.from_numpy(draws >= cells4.threshold(0.25))
+    dropped = (head.hidden.cpu() == 0) & (head.pre.cpu() > 0)
+    assert torch.equal(dropped.reshape(-1)[:400], ~kept & (head.pre.cpu().reshape(-1)[:400] > 0))
+    mask = (head.pre.cpu() > 0) & ~dropped
+    hidden = torch.where(mask, head.pre.double().cpu() / 0.75, 0.0)
+    close(head.hidden, hidden, hidden.abs(), 1)
+    h = values(head.layers[1].kept)
+    scores = h @ w1.t()
+    close(head.scores, scores, h.abs() @ w1.abs().t(), HIDDEN)
+    g = head.grad_scores.double().cpu()
+    close(head.layers[1].grad_weight, g.t() @ h, g.abs().t() @ h.abs(), 3 * cells)
+    gh = torch.where(mask, g @ w1 / 0.75, 0.0)
+    close(head.grad_hidden, gh, torch.where(mask, g.abs() @ w1.abs(), 0.0) / 0.75, 3 * CLASSES + 3)
+    g = head.grad_hidden.double().cpu()
+    close(head.layers[0].grad_weight, g.t() @ x, g.abs().t() @ x.abs(), 3 * cells)
+    close(head.layers[0].grad_bias, g.sum(0), g.abs().sum(0), cells)
+    close(head.grad_state, g @ w0, g.abs() @ w0.abs(), 3 * HIDDEN)
+
+
+def test_training_learns_the_same_every_time(gpu):
+    """Two heads of one seed make the same steps bit for bit; the state's gradient is
+    there for a backward through the automaton."""
+    state = final_state()
+    cells = state[..., 0].numel()
+    target = torch.randn(cells, CLASSES, device=gpu)
+    heads = [Head(cells, 5), Head(cells, 5)]
+    for head in heads:
+        for _ in range(4):
+            head.train(state, target)
+    for k in range(2):
+        assert torch.equal(heads[0].w[k], heads[1].w[k])
+        assert torch.equal(heads[0].b[k], heads[1].b[k])
+    assert torch.equal(heads[0].grad_state, heads[1].grad_state)
+    assert int(heads[0].step) == 4
+
+
+def test_captured_training_step(gpu):
+    """A training step captured into a graph and replayed, with eager work between the
+    replays: the same weights as eager steps, and another mask in every step."""
+    state = final_state()
+    cells = state[..., 0].numel()
+    target = torch.randn(cells, CLASSES, device=gpu)
+    eager, replayed = Head(cells, 9), Head(cells, 9)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for head in (eager, replayed):
+            head.train(state, target)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        replayed.train(state, target)
+    masks = []
+    for _ in range(4):
+        eager.train(state, target)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert torch.equal(eager.w[k], replayed.w[k])
+        assert torch.equal(eager.scores, replayed.scores)
+        masks.append((replayed.hidden == 0) & (replayed.pre > 0))
+    assert not any(torch.equal(a, b) for a, b in zip(masks, masks[1:]))
+
+
+def test_streams(gpu):
+    """A first call on another stream waits for what the constructors enqueued; two
+    layers on two streams at once."""
+    x = torch.randn(20000, 64, device=gpu)
+    w = torch.randn(70, 64, device=gpu)
+    want = CellLayer(w, rows=20000).forward(x, torch.zeros(20000, 70, device=gpu))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros(20000, 70, device=gpu) for _ in streams]
+    torch.cuda.synchronize()
+    busy = torch.randn(4096, 4096, device=gpu)
+    for _ in range(5):
+        busy = busy @ busy * 1e-3
+    layers = [CellLayer(w, rows=20000, train=True) for _ in streams]   # behind the products
+    for _ in range(3):
+        for layer, out, stream in zip(layers, outs, streams):
+            layer.forward(x, out, stream=stream)
+            layer.backward(out, stream=stream.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    assert torch.equal(layers[0].grad_weight, layers[1].grad_weight)
+
+
+def test_a_matrix_of_one_layer_in_another(gpu):
+    """Rows kept by one layer are read by others, at a time or together."""
+    x = torch.randn(3000, 200, device=gpu)
+    first = CellLayer(torch.randn(32, 200, device=gpu), rows=3000)
+    second = CellLayer(torch.randn(300, 200, device=gpu), rows=3000)
+    first.forward(x, torch.zeros(3000, 32, device=gpu))
+    a = second.forward(first.kept, torch.zeros(3000, 300, device=gpu))
+    b = second.forward(x, torch.zeros(3000, 300, device=gpu))
+    assert torch.equal(a, b)
+
+
+def test_refusals(gpu):
+    layer = CellLayer(torch.randn(20, 40, device=gpu), rows=30)
+    x, out = torch.zeros(30, 40, device=gpu), torch.zeros(30, 20, device=gpu)
+    for bad in (dict(x=torch.zeros(30, 41, device=gpu)), dict(x=x.double()), dict(x=x.cpu()),
+                dict(x=torch.zeros(40, 30, device=gpu).t()), dict(out=out[:29]),
+                dict(out=torch.zeros(1, 20, device=gpu).expand(30, 20)), dict(out=out.cpu()),
+                dict(x=MX4Matrix(30, 50)), dict(x=MX4Matrix(29, 40))):
+        with pytest.raises((octnca.OctreeNCAError, TypeError)):
+            layer.forward(bad.get("x", x), bad.get("out", out))
+    with pytest.raises(octnca.OctreeNCAError):
+        layer.backward(out)                       # made without memory for gradients
+    with pytest.raises(octnca.OctreeNCAError):
+        CellLayer(torch.randn(20, 40, device=gpu), torch.zeros(21, device=gpu),
+                  rows=30).forward(x, out)
+    with pytest.raises(octnca.OctreeNCAError):
+        CellLayer(torch.randn(40, device=gpu))
+    trained = CellLayer(torch.randn(20, 40, device=gpu), rows=30, train=True)
+    trained.forward(x, out)
+    for bad in (dict(grad_in=torch.zeros(30, 39, device=gpu)), dict(grad_in=x.half()),
+                dict(kept=MX4Matrix(31, 40))):
+        with pytest.raises(octnca.OctreeNCAError):
+            trained.backward(out, **bad)
