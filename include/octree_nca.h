@@ -626,7 +626,7 @@ typedef struct {
  * Rows from `rows` on up to the next multiple of 16 take up space; no call
  * writes them and no result depends on them. */
 typedef struct {
-    int64_t rows;    /* >= 0 */
+    int64_t rows;    /* 0 .. 2^29; of weights at most 2^20 */
     int64_t cols;    /* 1 .. 2^20 */
     void *codes;     /* octree_nca_mx4_code_bytes; 16-byte aligned */
     void *scales;    /* 1/16 of that; 16-byte aligned, outside codes */
@@ -701,7 +701,7 @@ typedef struct {
  * and x the gradient of out, it is their gradient (rate 0: of the ReLU alone).
  * out may be x, gate or add itself (same data and stride) and overlaps them not
  * otherwise.  What a dropped element holds does not matter.
- * Errors: EINVAL, ESHAPE, EHIP. */
+ * rows * cols is at most 2^44.  Errors: EINVAL, ESHAPE, EHIP. */
 int octree_nca_dropout(const octnca_dropout *dropout, const octnca_rows *x, const octnca_rows *gate,
                        const octnca_rows *add, const octnca_rows *out, int64_t rows, int64_t cols,
                        void *stream);

@@ -242,6 +242,16 @@ hipError_t launch_adamw(const octnca_param_list &l, const octnca_adamw &h, int64
 // Cell layers (mx4.hip, mx4_backward.hip, dropout.hip).  Sizes are checked;
 // rows > 0.
 inline int64_t mx4_blocks(int64_t cols) { return (cols + 31) / 32; }
+// Whether a result of i x j values is cut into tiles of 256 x 256 rather than 128 x 128:
+// where they fill the card and cover little more than the smaller ones.  us of the
+// product with large and small tiles: 196 large tiles (3584 x 4096 -> 3584) 52 and 72,
+// 100 of them (2560 x 4096 -> 2560) 46 and 36; gradients of 100000 x 300 <- 40, where
+// large ones cover 1.33 times as much, 62 and 52.
+inline bool mx4_large_tiles(int64_t i, int64_t j) {
+    const auto tiles = [](int64_t n, int64_t side) { return (n + side - 1) / side; };
+    const int64_t large = tiles(i, 256) * tiles(j, 256);
+    return large >= 192 && large * 16 <= tiles(i, 128) * tiles(j, 128) * 5;
+}
 hipError_t launch_mx4_quantise(const octnca_rows &x, const octnca_mx4 &m, hipStream_t stream);
 hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipStream_t stream);
 hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const float *bias,

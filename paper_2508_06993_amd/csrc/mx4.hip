@@ -205,7 +205,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows(ProductArgs p, const void
 
 // Tile of a workgroup among row_tiles x col_tiles.  Workgroups go round the eight dies,
 // each with its own L2: a die takes tiles in a row, which run down eight row tiles
-// before they go to the next columns.
+// before they go to the next columns.  us with this and with tiles in plain order, 4096
+// -> 4096: 512 rows 24 and 26, 1024 rows 26 and 27; large tiles: no difference.
 struct Tile {
     int row, col;
 };
@@ -431,9 +432,10 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
     });
 }
 
-// Which kernel serves a product that is not narrow.  Tiles of 256 x 256 where they
-// fill the card, tiles of 128 x 128 likewise, else a few rows at a time with the
-// columns split.
+// Which kernel serves a product that is not narrow: large tiles, tiles of 128 x 128
+// where there are 128 of them, else a few rows at a time with the columns split.  us of
+// tiles and of few rows, 4096 -> 4096: 512 rows (128 tiles) 24 and 22, 768 rows 25 and
+// 30, 1024 rows 26 and 39.
 namespace {
 
 template <typename V, typename X, int G>
@@ -466,7 +468,7 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
             return std::make_pair((a.rows + side - 1) / side, (w.rows + side - 1) / side);
         };
         const auto large = tiles(256), small = tiles(128);
-        if (large.first * large.second >= 192) {
+        if (mx4_large_tiles(a.rows, w.rows)) {
             product_tiles<V, 8, 2><<<(unsigned)(large.first * large.second), kThreads, 0, stream>>>(
                 p, (int)large.first, (int)large.second);
             return hipGetLastError();

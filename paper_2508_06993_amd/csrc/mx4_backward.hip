@@ -493,8 +493,8 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
         }
 }
 
-// to[e] = sum of from[s][e] over the splits s, of two lists; a wave takes every
-// kJoin-th split of 64 elements, and the waves' sums are added in order.
+// to[e] = sum of from[s][e] over the splits s, of two lists.  Many splits: a wave takes
+// every kJoin-th split of 64 elements, and the waves' sums are added in order.
 constexpr int kJoin = 16;
 struct JoinArgs {
     const float *from[2];
@@ -521,13 +521,19 @@ __global__ __launch_bounds__(64 * kJoin) void join(JoinArgs a) {
     }
 }
 
-constexpr int kLarge = 4, kSmall = 2;   // I of the two tile sizes
-
-// Whether a result of i x j values is cut into large tiles: where they fill the card.
-bool large_tiles(int64_t i, int64_t j) {
-    constexpr int64_t kSide = 64 * kLarge;
-    return j > kSide / 2 && ((i + kSide - 1) / kSide) * ((j + kSide - 1) / kSide) >= 192;
+// Few splits: a thread takes an element.
+__global__ __launch_bounds__(kThreads) void join_few(JoinArgs a) {
+    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < a.n[0] + a.n[1];
+         e += (int64_t)gridDim.x * kThreads) {
+        const int which = e >= a.n[0];
+        const int64_t at = which ? e - a.n[0] : e;
+        double x = 0.0;
+        for (int s = 0; s < a.splits; ++s) x += a.from[which][s * a.n[which] + at];
+        a.to[which][at] = (float)x;
+    }
 }
+
+constexpr int kLarge = 4, kSmall = 2;   // I of the two tile sizes
 
 // Sizes of the narrow kernel for a layer; nt 0: it is too wide.
 struct Narrow {
@@ -540,14 +546,17 @@ Narrow narrow_of(int64_t cols, int64_t outs) {
     return Narrow{nt, kt};
 }
 
-// Splits of the rows for grad_weight.
+// Splits of the rows for grad_weight: as many as fill the card.
 int splits_of(int64_t rows, int64_t cols, int64_t outs) {
     const int64_t most = std::max<int64_t>(1, (rows + 127) / 128);
     if (narrow_of(cols, outs).nt) return (int)std::min<int64_t>(512, most);
-    const bool large = large_tiles(outs, cols);
+    const bool large = mx4_large_tiles(outs, cols);
     const int64_t side = 64 * (large ? kLarge : kSmall);
     const int64_t tiles = ((cols + side - 1) / side) * ((outs + side - 1) / side);
-    return (int)std::min(((large ? 256 : 512) + tiles - 1) / tiles, (most + 1) / 2);
+    // two workgroups of small tiles a compute unit; one split where the tiles alone fill
+    // the card
+    const int64_t want = tiles >= 192 ? 1 : ((large ? 256 : 512) + tiles - 1) / tiles;
+    return (int)std::min(want, (most + 1) / 2);
 }
 
 size_t sums_bytes(int64_t splits, int64_t cols, int64_t outs) {
@@ -570,7 +579,7 @@ void run_tiles(BackwardArgs b, int splits, bool products, hipStream_t stream) {
 
 template <typename V, bool WEIGHT>
 void run(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
-    if (large_tiles(WEIGHT ? b.outs : b.rows, b.cols))
+    if (mx4_large_tiles(WEIGHT ? b.outs : b.rows, b.cols))
         run_tiles<V, WEIGHT, kLarge>(b, splits, products, stream);
     else
         run_tiles<V, WEIGHT, kSmall>(b, splits, products, stream);
@@ -657,7 +666,11 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
             const int64_t n0 = grad_weight ? outs * cols : 0, n1 = grad_bias ? outs : 0;
             JoinArgs j{{sums, bias_sums}, {grad_weight, grad_bias}, {n0, n1}, (n0 + 63) / 64,
                        splits};
-            join<<<(unsigned)(j.blocks + (n1 + 63) / 64), 64 * kJoin, 0, stream>>>(j);
+            if (splits > kJoin)
+                join<<<(unsigned)(j.blocks + (n1 + 63) / 64), 64 * kJoin, 0, stream>>>(j);
+            else
+                join_few<<<(unsigned)std::min<int64_t>((n0 + n1 + kThreads - 1) / kThreads, 1 << 14),
+                           kThreads, 0, stream>>>(j);
         }
         return hipGetLastError();
     });

@@ -314,8 +314,12 @@ class MX4Matrix:
 
     def quantise(self, x: torch.Tensor, stream=None) -> "MX4Matrix":
         """Takes x [...][cols], of fp32, fp16 or bf16."""
-        self.used = x.numel() // self.cols
-        octree_nca_mx4_quantise(x, self.struct, self._own.use(stream))
+        before, self.used = self.used, x.numel() // self.cols
+        try:
+            octree_nca_mx4_quantise(x, self.struct, self._own.use(stream))
+        except Exception:      # refused: nothing has been written
+            self.used = before
+            raise
         return self
 
     def dequantise(self, out: torch.Tensor, stream=None) -> torch.Tensor:
@@ -370,8 +374,13 @@ class CellLayer:
             octree_nca_mx4_product(x.struct, self.w.struct, out, self.bias, relu,
                                    x._own.use(stream))
         else:
-            self.kept.used = x.numel() // self.cols
-            octree_nca_mx4_linear(x, self.kept.struct, self.w.struct, out, self.bias, relu, stream)
+            kept = self.kept
+            before, kept.used = kept.used, x.numel() // self.cols
+            try:
+                octree_nca_mx4_linear(x, kept.struct, self.w.struct, out, self.bias, relu, stream)
+            except Exception:      # refused: nothing has been written
+                kept.used = before
+                raise
         return out
 
     def backward(self, grad_out: torch.Tensor, grad_in: Optional[torch.Tensor] = None,

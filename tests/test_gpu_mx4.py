@@ -344,6 +344,29 @@ def test_fewer_rows_than_room(gpu):
         layer.forward(torch.zeros(501, 40, device=gpu), torch.zeros(501, 20, device=gpu))
     with pytest.raises(octnca.OctreeNCAError):   # not the rows of the last forward
         layer.backward(torch.zeros(36, 20, device=gpu))
+    # a refused call leaves the last forward's rows
+    with pytest.raises(octnca.OctreeNCAError):
+        layer.forward(torch.zeros(5, 40, device=gpu), torch.zeros(4, 20, device=gpu))
+    with pytest.raises(octnca.OctreeNCAError):
+        layer.kept.quantise(torch.zeros(5, 41, device=gpu))
+    assert layer.kept.used == 37
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(5, 40, 20), (5, 300, 200), (37, 300, 200),
+                                            (1100, 40, 20), (5003, 200, 1500)])
+def test_memory_past_the_rows_is_left(gpu, rows, cols, outs):
+    """The input's codes, however the product is made, and the outputs' buffer."""
+    layer = CellLayer(torch.randn(outs, cols, device=gpu), rows=rows)
+    codes, scales = layer.kept.buffers.codes, layer.kept.buffers.scales
+    codes.fill_(0xA5)
+    scales.fill_(0x5A)
+    out = torch.full((rows + 3, outs), 7.0, device=gpu)
+    layer.forward(torch.randn(rows, cols, device=gpu), out[:rows])
+    past = torch.arange(codes.shape[0] * 16, device=gpu).reshape(-1, 1, 16) >= rows
+    past = past.expand(scales.shape)
+    assert (scales[past] == 0x5A).all() and (codes[past] == 0xA5).all()
+    assert (scales[~past] != 0x5A).all() and (out[rows:] == 7).all()
+    assert torch.equal(values_of(layer.kept).isfinite().all(), torch.tensor(True, device=gpu))
 
 
 def test_states_and_images_as_rows(gpu):
