@@ -1,4 +1,10 @@
 // Dropout whose mask is drawn where it is used (formulas in octree_nca.h).
+//
+// One pass over memory: 131072 x 4096 bf16 with an addend (3.2 GB) 537 us, 6.0 TB/s;
+// 102403 x 517 fp16 gated, rows 520 apart (318 MB), 64 us, 4.9 TB/s.  The generator is
+// the 4 x 32 variant because its twenty 32-bit products give four draws, where the fire
+// mask's 4 x 64 variant needs eighty for eight: at two bytes an element that would take
+// longer than the memory.
 #include <algorithm>
 #include <type_traits>
 

