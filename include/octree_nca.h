@@ -673,7 +673,7 @@ size_t octree_nca_mx4_backward_workspace_bytes(int64_t rows, int64_t cols, int64
  *   workspace    16-byte aligned; NULL is allowed without grad_weight and grad_bias.
  * Written arrays lie outside each other and outside what is read, and are
  * overwritten (rows = 0: with zeros).  The products take every bit of G (as sums of
- * bf16 values; what of it lies below 2^-126 may be lost), are summed in fp32 and in
+ * bf16 values; what of them, of a and of w lies below 2^-126 may be lost), are summed in fp32 and in
  * an order that depends on the sizes only.
  * Errors: EINVAL, ESHAPE, ESPACE, EHIP. */
 int octree_nca_mx4_backward(const octnca_rows *grad_out, const octnca_mx4 *a, const octnca_mx4 *w,

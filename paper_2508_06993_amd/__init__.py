@@ -852,9 +852,9 @@ def octree_nca_adamw(plist: _ParamList, step, lr: float, betas=(0.9, 0.99), eps=
 
 def _on_device(t, name):
     """Refuses tensors that the current device's kernels would not be given."""
-    if not t.is_cuda:
-        raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
-    if t.device.index != _current_device():
+    if t.get_device() != _current_device():
+        if not t.is_cuda:
+            raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
         raise OctreeNCAError(f"{name}: on {t.device}, the current device is {_current_device()}")
 
 

@@ -70,25 +70,13 @@ inline Mx4View mx4_view(const octnca_mx4 &m) {
                    (int)((m.cols + kMxBlock - 1) / kMxBlock)};
 }
 
-// A lane's part of 16 rows times four blocks (128 columns): row lane % 16 of the
-// group, block lane / 16 of the four, as the matrix instruction wants it.  The
-// four blocks of a group are 1 KB in a row.
+// A lane's part of an operand: a block of a row.  For the instruction of 16 rows and
+// four blocks (128 columns) row lane % 16 of a group, block lane / 16 of the four,
+// which lie in memory as one KB.
 struct Mx4Operand {
     Words4 codes;
     uint32_t scale;
 };
-
-// Blocks past the last have codes 0 and scale 1.
-__device__ __forceinline__ Mx4Operand mx4_operand(const Mx4View &m, int64_t group, int block) {
-    const int lane = threadIdx.x & 63;
-    const int64_t at = (group * m.blocks + block) * kMxGroup + lane;
-    Mx4Operand o{Words4{0, 0, 0, 0}, 127};
-    if (block + lane / kMxGroup < m.blocks) {
-        o.codes = ((const Words4 *)m.codes)[at];
-        o.scale = m.scales[at];
-    }
-    return o;
-}
 
 // acc[i] of lane l += sum over 128 columns of a's row 4 (l / 16) + i times b's row
 // l % 16.
@@ -111,7 +99,7 @@ __device__ __forceinline__ v16f32 mx4_mfma32(const Mx4Operand &a, const Mx4Opera
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 4, 4, 0, a.scale, 0, b.scale);
 }
 
-// x of lane K of each four lanes; of the lane's partner in them.
+// x of lane K of each four lanes; the largest of the four.
 template <int K> __device__ __forceinline__ uint32_t quad_lane(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, K * 0x55, 15, 15, true);
 }

@@ -1,4 +1,4 @@
-// Rows of fp32, fp16 and bf16 values: one or eight consecutive ones as fp32.
+// Rows of fp32, fp16 and bf16 values: one, four or eight consecutive ones as fp32.
 // Internal header (not part of the ABI).
 #pragma once
 
@@ -25,14 +25,6 @@ template <> struct Values<OCTNCA_F32> {
     static constexpr int kBytes = 4;
     static __device__ __forceinline__ float get(const T *p) { return *p; }
     static __device__ __forceinline__ void put(T *p, float x) { *p = x; }
-    static __device__ __forceinline__ void get8(const T *p, float *x) {
-        const Words4 a = ((const Words4At4 *)p)[0], b = ((const Words4At4 *)p)[1];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] = __uint_as_float(a[k]);
-            x[k + 4] = __uint_as_float(b[k]);
-        }
-    }
     template <bool STREAM = false>
     static __device__ __forceinline__ void put8(T *p, const float *x) {
         Words4 a, b;
@@ -61,11 +53,6 @@ template <typename H> struct Values16 {
     typedef H H8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ float get(const T *p) { return (float)*p; }
     static __device__ __forceinline__ void put(T *p, float x) { *p = (T)x; }
-    static __device__ __forceinline__ void get8(const T *p, float *x) {
-        const H8 a = __builtin_bit_cast(H8, *(const Words4At2 *)p);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = (float)a[k];
-    }
     template <bool STREAM = false>
     static __device__ __forceinline__ void put8(T *p, const float *x) {
         H8 a;

@@ -376,3 +376,41 @@ def test_states_and_images_as_rows(gpu):
     a = layer.forward(state, torch.zeros(1, 12, 20, 5, device=gpu))
     b = layer.forward(state.reshape(240, 16), torch.zeros(240, 5, device=gpu))
     assert torch.equal(a.reshape(240, 5), b)
+
+
+def test_far_rows(gpu):
+    """Codes and values past 2^32 bytes: the last rows as in a matrix of their own."""
+    rows, cols, few = 4_300_003, 2100, 83          # codes 4.5 GB, values 18 GB
+    first = rows // 16 * 16 - 64                   # whole row groups before the last ones
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device=gpu)
+    x[:1000].normal_()
+    x[1000:first] = 0
+    x[first:].normal_()
+    layer = CellLayer(torch.randn(20, cols, device=gpu), rows=rows, train=True)
+    assert layer.kept.buffers.codes.numel() > 2 ** 32
+    alone = CellLayer(layer.weight, rows=few, train=True)
+    out = layer.forward(x, torch.empty((rows, 20), device=gpu))
+    last, n = x[first:], rows - first
+    want = alone.forward(last, torch.empty((n, 20), device=gpu))
+    a, v = values_of(alone.kept), values_of(alone.w)
+    groups = layer.kept.buffers.codes[first // 16:], layer.kept.buffers.scales[first // 16:]
+    assert torch.equal(groups[0][:4], alone.kept.buffers.codes[:4])
+    assert torch.equal(groups[1][:4], alone.kept.buffers.scales[:4])
+    exact = a @ v.t()
+    bound = sum_bound(cols, a.abs() @ v.abs().t(), exact, "f32")
+    check(out[first:], exact, bound)
+    check(want, exact, bound)
+    assert (out[1000:first] == 0).all()
+    back = layer.kept.dequantise(torch.empty_like(x))
+    assert torch.equal(back[first:].double(), a) and (back[1000:first] == 0).all()
+    del back
+    g = torch.zeros((rows, 20), device=gpu)
+    g[first:].normal_()
+    grad_in = torch.empty_like(x, dtype=torch.float32)
+    layer.backward(g, grad_in)
+    gd = g[first:].double()
+    exact = gd @ v
+    check(grad_in[first:], exact, sum_bound(60, gd.abs() @ v.abs(), exact, "f32"))
+    assert (grad_in[:first] == 0).all()
+    exact = gd.t() @ a     # the other rows' terms are zeros
+    check(layer.grad_weight, exact, sum_bound(3 * n + 512, gd.abs().t() @ a.abs(), exact, "f32"))
