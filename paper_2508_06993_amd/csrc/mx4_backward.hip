@@ -7,14 +7,15 @@
 // the matrix instructions.
 //
 // Wide layers are bound by the matrix cores and by what feeds them: 8192 x 4096 <- 4096
-// in bf16 takes 320 us for grad_in and 346 for grad_weight (860 and 790 TFLOP/s; a
-// library's bf16 product of 8192^3 reaches 1340, these instructions alone about 1500).
+// in bf16 takes 289 us for grad_in and 333 for grad_weight under the profiler, 561 in
+// all without (980 TFLOP/s; a library's bf16 product of 8192^3 reaches 1340).
 // Both operands need the summed index along the rows of LDS tiles, so they are
 // written row by row and read transposed.  What took it from 6069 us: transposed reads
 // and tiles of 256 x 256 (802), no use of a loaded value before the products that
-// cover its way (724), 32 x 32 instructions and the work for LDS between them (592).
+// cover its way (724), 32 x 32 instructions and the work for LDS between them (592),
+// codes to bf16 with their scale in one instruction (551 to 561).
 // Narrow layers are bound by memory: one pass over G gives all three.  320 x 320
-// cells, 32 <- 64 in fp32 (41 MB): 17.1 us and 3.9 for joining the splits; as two
+// cells, 32 <- 64 in fp32 (41 MB): 16.6 us and 3.9 for joining the splits; as two
 // passes on tiles it was 46, 27 and 6.
 #include <algorithm>
 #include <type_traits>
@@ -164,16 +165,14 @@ template <typename V, bool WHOLE> struct Raw8 {
     }
 };
 
-// Eight codes as bf16 values (exact).
+// Eight codes as bf16 values (exact: a code has two significant bits).
 __device__ __forceinline__ Words4 code_values(uint32_t codes, uint32_t scale) {
     const float s = mx4_scale_value(scale);
     Words4 out;
-    float v[8];
-    mx4_values(codes, v);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        out[k] = __float_as_uint(v[2 * k] * s) >> 16 |
-                 (__float_as_uint(v[2 * k + 1] * s) & 0xffff0000u);
+    out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
+    out[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
+    out[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
     return out;
 }
 

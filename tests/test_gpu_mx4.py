@@ -277,6 +277,36 @@ def test_backward_values_that_are_not_finite(gpu):
         assert ((got.double() - want)[ok].abs() <= 1e-4 * (1 + want[ok].abs())).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,outs", [(300, 70, 40), (300, 300, 200), (300, 3500, 3700)])
+def test_backward_with_odd_blocks(gpu, rows, cols, outs, dtype):
+    """Blocks of NaN reach the gradients of their columns and no others; blocks of the
+    smallest and of large scales are exact."""
+    w, x = torch.randn(outs, cols, device=gpu), torch.randn(rows, cols, device=gpu)
+    w[3, :32] *= 2.0 ** -126       # scale 2^-127: what is left of it is below 2^-124
+    x[5, 32:64] *= 2.0 ** 100
+    w[outs - 1, cols - 1] = float("nan")
+    x[rows - 1, 33] = float("inf")
+    layer = CellLayer(w, rows=rows, train=True)
+    layer.kept.quantise(x)
+    g = torch.randn(rows, outs, device=gpu).to(TYPES[dtype])
+    grad_in = torch.zeros((rows, cols), dtype=TYPES[dtype], device=gpu)
+    layer.backward(g, grad_in)
+    a, v, gd = values_of(layer.kept), values_of(layer.w), g.double()
+    nan_in = torch.zeros(cols, dtype=torch.bool, device=gpu)
+    nan_in[(cols - 1) // 32 * 32:] = True
+    nan_w = torch.zeros(cols, dtype=torch.bool, device=gpu)
+    nan_w[32:64] = True
+    assert torch.equal(grad_in.isnan(), nan_in.expand(rows, cols))
+    assert torch.equal(layer.grad_weight.isnan(), nan_w.expand(outs, cols))
+    want = (gd @ v.nan_to_num())[:, ~nan_in]
+    check(grad_in[:, ~nan_in], want,
+          sum_bound(3 * outs, (gd.abs() @ v.nan_to_num().abs())[:, ~nan_in], want, dtype))
+    want = (gd.t() @ a.nan_to_num())[:, ~nan_w]
+    check(layer.grad_weight[:, ~nan_w], want,
+          sum_bound(3 * rows, (gd.abs().t() @ a.nan_to_num().abs())[:, ~nan_w], want, "f32"))
+
+
 def test_gradients_by_differences(gpu):
     """grad_weight and grad_in against difference quotients of the product itself:
     it is linear in each code's value, and steps of whole values keep the scales."""
