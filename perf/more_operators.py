@@ -182,7 +182,10 @@ def prepare(case, seed):
         elif call == "dropout":
             st["drop"] = Dropout(case["rate"], st["seed"])
         else:
-            st["layer"] = CellLayer(st["w"], st["bias"], rows=rows, train=call == "backward")
+            bias = st["bias"]
+            if call == "backward":      # a layer without a bias has no gradient of it
+                bias = torch.zeros(case["outs"], device="cuda")
+            st["layer"] = CellLayer(st["w"], bias, rows=rows, train=call == "backward")
             if "kept" in st:
                 st["mx"] = MX4Matrix(rows, cols).quantise(st["kept"])
     st["case"] = case
