@@ -347,6 +347,7 @@ class CellLayer:
         self.outs, self.cols = weight.shape
         self.w = MX4Matrix(self.outs, self.cols, device=weight.device)
         self.kept = MX4Matrix(rows, self.cols, device=weight.device)
+        self.last = self.kept      # what the last forward has multiplied
         self.grad_weight = self.grad_bias = self.workspace = None
         own = [self.w.buffers.codes, self.w.buffers.scales, self.kept.buffers.codes,
                self.kept.buffers.scales]
@@ -373,6 +374,7 @@ class CellLayer:
         if isinstance(x, MX4Matrix):
             octree_nca_mx4_product(x.struct, self.w.struct, out, self.bias, relu,
                                    x._own.use(stream))
+            self.last = x
         else:
             kept = self.kept
             before, kept.used = kept.used, x.numel() // self.cols
@@ -381,20 +383,20 @@ class CellLayer:
             except Exception:      # refused: nothing has been written
                 kept.used = before
                 raise
+            self.last = kept
         return out
 
     def backward(self, grad_out: torch.Tensor, grad_in: Optional[torch.Tensor] = None,
                  kept: Optional[MX4Matrix] = None, stream=None) -> None:
         """Fills ``grad_weight`` and ``grad_bias``, and grad_in [...][cols] (of
         grad_out's type) if given, for the gradient of the last forward's out
-        (without its relu), or of that of the rows ``kept``."""
+        (without its relu), or of the product of the rows ``kept``."""
         if self.workspace is None:
             raise OctreeNCAError("CellLayer: made without train=True")
         stream = self._own.use(stream)
-        if kept is not None:
-            kept._own.use(stream)
-        octree_nca_mx4_backward(grad_out, (kept or self.kept).struct, self.w.struct, grad_in,
-                                self.grad_weight, self.grad_bias, self.workspace, stream)
+        rows = self.last if kept is None else kept
+        octree_nca_mx4_backward(grad_out, rows.struct, self.w.struct, grad_in, self.grad_weight,
+                                self.grad_bias, self.workspace, rows._own.use(stream))
 
 
 class Dropout:

@@ -181,6 +181,20 @@ def test_a_matrix_of_one_layer_in_another(gpu):
     a = second.forward(first.kept, torch.zeros(3000, 300, device=gpu))
     b = second.forward(x, torch.zeros(3000, 300, device=gpu))
     assert torch.equal(a, b)
+    # a backward takes what the last forward has multiplied
+    third = CellLayer(second.weight, rows=5, train=True)
+    third.kept.quantise(torch.randn(5, 200, device=gpu))
+    g = torch.randn(3000, 300, device=gpu)
+    with pytest.raises(octnca.OctreeNCAError):       # memory for the gradients of 5 rows
+        third.backward(g, kept=first.kept)
+    third = CellLayer(second.weight, rows=3000, train=True)
+    third.forward(x, a)
+    third.backward(g)
+    want = third.grad_weight.clone()
+    third.forward(torch.randn(7, 200, device=gpu), torch.zeros(7, 300, device=gpu))
+    third.forward(first.kept, a)
+    third.backward(g)
+    assert torch.equal(third.grad_weight, want)
 
 
 def test_refusals(gpu):
