@@ -123,7 +123,10 @@ SIZES = [  # rows, cols, outs: one cell, few, many; parts of blocks and groups
     (1, 1, 1), (1, 32, 16), (1, 4096, 64), (1, 1000, 1003), (2, 517, 33), (5, 64, 300),
     (16, 2048, 100), (17, 96, 16), (33, 128, 129), (64, 33, 2), (100, 300, 70), (257, 128, 256),
     (300, 1024, 520), (1000, 16, 19), (1031, 20, 100), (5000, 32, 64), (3001, 40, 3),
-    (20011, 64, 16), (4099, 100, 20), (513, 640, 600), (70001, 32, 2)]
+    (20011, 64, 16), (4099, 100, 20), (513, 640, 600), (70001, 32, 2),
+    # each way to share few rows out; as many values as a workgroup quantises, and more
+    (40, 1000, 300), (20, 1000, 300), (20, 1100, 4099), (50, 1100, 4099), (5, 5, 300),
+    (3, 7, 1000), (16, 1024, 300), (17, 1024, 300), (15, 1056, 300), (200, 3, 140)]
 
 
 @pytest.mark.parametrize("rows,cols,outs", SIZES)
@@ -190,7 +193,9 @@ def test_no_rows(gpu):
 @pytest.mark.parametrize("rows,cols,outs", [(1, 1, 1), (1, 100, 30), (2, 517, 33), (17, 96, 16),
                                             (63, 33, 65), (100, 300, 70), (1000, 16, 19),
                                             (1031, 20, 100), (5003, 32, 64), (20011, 64, 16),
-                                            (700, 640, 600), (130, 1100, 257), (40000, 40, 3)])
+                                            (700, 640, 600), (130, 1100, 257), (40000, 40, 3),
+                                            (3, 9, 7), (50, 130, 5), (633, 10, 925),
+                                            (2000, 128, 60), (2000, 60, 128), (999, 128, 128)])
 def test_backward(gpu, rows, cols, outs, dtype):
     gen = torch.Generator(device=gpu).manual_seed(rows * 5 + cols + outs)
     g = torch.randn(rows, outs, generator=gen, device=gpu)
