@@ -852,9 +852,10 @@ def octree_nca_adamw(plist: _ParamList, step, lr: float, betas=(0.9, 0.99), eps=
 
 def _on_device(t, name):
     """Refuses tensors that the current device's kernels would not be given."""
-    if t.get_device() != _current_device():
-        if not t.is_cuda:
-            raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
+    device = t.get_device()
+    if device < 0:
+        raise OctreeNCAError(f"{name}: must be a device (cuda) tensor")
+    if device != _current_device():
         raise OctreeNCAError(f"{name}: on {t.device}, the current device is {_current_device()}")
 
 

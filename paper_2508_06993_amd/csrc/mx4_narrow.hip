@@ -97,9 +97,9 @@ __device__ __forceinline__ void put_group(const NarrowArgs &b, int64_t group, co
 }
 
 // A wave takes four units (a block of a row group each) at a time: 64 / KB rows, the
-// next ones being loaded meanwhile.  The matrix instruction multiplies 16 rows of four blocks; where rows
-// have fewer, the blocks of other rows are blanked: one instruction a row group.
-// V: type of the values, or int: codes.
+// next ones being loaded meanwhile.  The matrix instruction multiplies 16 rows of four
+// blocks; where rows have fewer, the blocks of other rows are blanked: one instruction
+// a row group.  V: type of the values, or int: codes.
 template <typename V, int KB, int NT>
 __global__ __launch_bounds__(kThreads) void narrow(NarrowArgs b) {
     constexpr bool kValues = !std::is_same<V, int>::value;

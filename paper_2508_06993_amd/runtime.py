@@ -11,15 +11,15 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (Model, MX4Buffers, OctreeNCAError, StateCacheBuffers, _stream, _cache_call, check_train_weights,
-               lib, octree_nca_adamw, octree_nca_clip_grads, octree_nca_dropout, octree_nca_grad_norm,
-               octree_nca_infer, octree_nca_mx4_backward,
-               octree_nca_mx4_backward_workspace_bytes, octree_nca_mx4_dequantise,
-               octree_nca_mx4_linear, octree_nca_mx4_product, octree_nca_mx4_quantise,
-               octree_nca_param_table, octree_nca_param_table_bytes,
+from . import (Model, MX4Buffers, OctreeNCAError, StateCacheBuffers, _stream, _cache_call,
+               check_train_weights, lib, mx4_shapes, octree_nca_adamw, octree_nca_clip_grads,
+               octree_nca_dropout, octree_nca_grad_norm, octree_nca_infer,
+               octree_nca_mx4_backward, octree_nca_mx4_backward_workspace_bytes,
+               octree_nca_mx4_dequantise, octree_nca_mx4_linear, octree_nca_mx4_product,
+               octree_nca_mx4_quantise, octree_nca_param_table, octree_nca_param_table_bytes,
                octree_nca_train_kept_workspace_bytes, octree_nca_train_step,
                octree_nca_train_step_kept, octree_nca_train_workspace_bytes,
-               octree_nca_workspace_bytes, param_structs, state_cache_refs, mx4_shapes)
+               octree_nca_workspace_bytes, param_structs, state_cache_refs)
 
 WEIGHT_FIELDS = ("conv_w", "conv_b", "w1", "b1", "w2")
 
