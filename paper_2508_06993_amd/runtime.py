@@ -96,7 +96,8 @@ class _Buffers:
 
     def __init__(self, *tensors):
         self.tensors = tensors
-        self.streams = {_stream(None)}
+        self.streams = {_stream(None)}     # that torch keeps the memory for
+        self.waited = set(self.streams)    # that come after the fills
         # within a capture the graph has its own order
         self.filled = None if torch.cuda.is_current_stream_capturing() else torch.cuda.Event()
         if self.filled is not None:
@@ -105,7 +106,7 @@ class _Buffers:
     def use(self, stream) -> int:
         """Handle of the stream of a call."""
         handle = _stream(stream)
-        if handle not in self.streams:
+        if handle not in (self.waited if type(stream) is int else self.streams):
             self._first_use(stream, handle)
         return handle
 
@@ -116,11 +117,13 @@ class _Buffers:
             return
         if stream is None:
             stream = torch.cuda.current_stream()
-        _torch_stream(stream).wait_event(self.filled)
+        if handle not in self.waited:
+            _torch_stream(stream).wait_event(self.filled)
+            self.waited.add(handle)
         if isinstance(stream, torch.cuda.Stream):
             for t in self.tensors:
                 t.record_stream(stream)
-        self.streams.add(handle)
+            self.streams.add(handle)
 
 
 class StateCache:
@@ -370,16 +373,16 @@ class CellLayer:
     def forward(self, x, out: torch.Tensor, relu=False, stream=None) -> torch.Tensor:
         """Fills and returns ``out`` [...][outs].  x: [...][cols], left in 4 bits in
         ``kept``; or an MX4Matrix of such rows."""
-        stream = self._own.use(stream)
+        handle = self._own.use(stream)
         if isinstance(x, MX4Matrix):
-            octree_nca_mx4_product(x.struct, self.w.struct, out, self.bias, relu,
-                                   x._own.use(stream))
+            x._own.use(stream)
+            octree_nca_mx4_product(x.struct, self.w.struct, out, self.bias, relu, handle)
             self.last = x
         else:
             kept = self.kept
             before, kept.used = kept.used, x.numel() // self.cols
             try:
-                octree_nca_mx4_linear(x, kept.struct, self.w.struct, out, self.bias, relu, stream)
+                octree_nca_mx4_linear(x, kept.struct, self.w.struct, out, self.bias, relu, handle)
             except Exception:      # refused: nothing has been written
                 kept.used = before
                 raise
@@ -393,10 +396,11 @@ class CellLayer:
         (without its relu), or of the product of the rows ``kept``."""
         if self.workspace is None:
             raise OctreeNCAError("CellLayer: made without train=True")
-        stream = self._own.use(stream)
+        handle = self._own.use(stream)
         rows = self.last if kept is None else kept
+        rows._own.use(stream)
         octree_nca_mx4_backward(grad_out, rows.struct, self.w.struct, grad_in, self.grad_weight,
-                                self.grad_bias, self.workspace, rows._own.use(stream))
+                                self.grad_bias, self.workspace, handle)
 
 
 class Dropout:
