@@ -160,6 +160,7 @@ class _Rows(ctypes.Structure):
 class _MX4(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p),
                 ("scales", ctypes.c_void_p)]
+    device = None    # its memory's; None: not known
 
 
 class _Dropout(ctypes.Structure):
@@ -859,6 +860,16 @@ def _on_device(t, name):
         raise OctreeNCAError(f"{name}: on {t.device}, the current device is {_current_device()}")
 
 
+def _here(*matrices):
+    """Refuses matrices in 4 bits whose memory the current device's kernels would not be
+    given."""
+    device = _current_device()
+    for m in matrices:
+        if m.device is not None and m.device != device:
+            raise OctreeNCAError(f"matrix in 4 bits: on cuda:{m.device}, the current device is "
+                                 f"{device}")
+
+
 def _rows(t, name, rows=None, cols=None):
     """octnca_rows of a tensor [..., cols]: rows any distance apart (two
     dimensions) or contiguous; checked against a size if one is given."""
@@ -917,8 +928,10 @@ class MX4Buffers:
             if shape[1:] != want[1:] or len(shape) != len(want) or shape[0] < want[0]:
                 raise OctreeNCAError(f"{name}: expected shape {want}, got {shape}")
             _on_device(t, name)
-        return _MX4(self.rows, self.cols, _ptr(self.codes, torch.uint8, "codes"),
-                    _ptr(self.scales, torch.uint8, "scales"))
+        m = _MX4(self.rows, self.cols, _ptr(self.codes, torch.uint8, "codes"),
+                 _ptr(self.scales, torch.uint8, "scales"))
+        m.device = self.codes.get_device()
+        return m
 
 
 def octree_nca_mx4_code_bytes(rows: int, cols: int) -> int:
@@ -927,6 +940,7 @@ def octree_nca_mx4_code_bytes(rows: int, cols: int) -> int:
 
 def octree_nca_mx4_quantise(x, m: _MX4, stream=None) -> None:
     """m (MX4Buffers.struct) = x [rows][cols] in 4 bits."""
+    _here(m)
     st = lib().octree_nca_mx4_quantise(_rows(x, "x", m.rows, m.cols)[0], m, _stream(stream))
     if st:
         _check(st, "octree_nca_mx4_quantise")
@@ -934,6 +948,7 @@ def octree_nca_mx4_quantise(x, m: _MX4, stream=None) -> None:
 
 def octree_nca_mx4_dequantise(m: _MX4, x, stream=None) -> None:
     """x [rows][cols] = the values of m."""
+    _here(m)
     st = lib().octree_nca_mx4_dequantise(m, _rows(x, "x", m.rows, m.cols)[0], _stream(stream))
     if st:
         _check(st, "octree_nca_mx4_dequantise")
@@ -941,6 +956,7 @@ def octree_nca_mx4_dequantise(m: _MX4, x, stream=None) -> None:
 
 def octree_nca_mx4_product(a: _MX4, w: _MX4, out, bias=None, relu=False, stream=None) -> None:
     """out [a.rows][w.rows] = a times w transposed, plus bias; relu."""
+    _here(a, w)
     st = lib().octree_nca_mx4_product(a, w, _vector(bias, "bias", w.rows), relu,
                                       _rows(out, "out", a.rows, w.rows)[0], _stream(stream))
     if st:
@@ -950,6 +966,7 @@ def octree_nca_mx4_product(a: _MX4, w: _MX4, out, bias=None, relu=False, stream=
 def octree_nca_mx4_linear(x, kept: _MX4, w: _MX4, out, bias=None, relu=False,
                           stream=None) -> None:
     """kept = x in 4 bits, out = kept times w transposed, plus bias; relu."""
+    _here(kept, w)
     st = lib().octree_nca_mx4_linear(_rows(x, "x", kept.rows, kept.cols)[0], kept, w,
                                      _vector(bias, "bias", w.rows), relu,
                                      _rows(out, "out", kept.rows, w.rows)[0], _stream(stream))
@@ -965,6 +982,7 @@ def octree_nca_mx4_backward(grad_out, a: _MX4, w: _MX4, grad_in=None, grad_weigh
                             grad_bias=None, workspace=None, stream=None) -> None:
     """Gradients of the product of a and w for the gradient grad_out
     [a.rows][w.rows]; grad_weight fp32 [w.rows][a.cols], grad_bias fp32 [w.rows]."""
+    _here(a, w)
     if workspace is not None:
         _on_device(workspace, "workspace")
     st = lib().octree_nca_mx4_backward(
