@@ -642,8 +642,10 @@ void run_narrow(const NarrowArgs &b, Narrow size, bool whole, int splits, hipStr
 }  // namespace
 
 size_t mx4_backward_bytes(int64_t rows, int64_t cols, int64_t outs) {
-    // as a call of any fewer rows needs, too
-    return std::max<size_t>(16, sums_bytes(splits_of(rows, cols, outs), cols, outs));
+    // One split's sums are the gradients themselves.  Fewer rows never have more splits,
+    // so they need no more.
+    const int splits = splits_of(rows, cols, outs);
+    return splits == 1 ? 16 : std::max<size_t>(16, sums_bytes(splits, cols, outs));
 }
 
 hipError_t launch_mx4_backward(const octnca_rows &grad_out, const octnca_mx4 &a,
