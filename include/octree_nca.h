@@ -607,7 +607,9 @@ int octree_nca_adamw(const octnca_param_list *list, const octnca_adamw *settings
  *   and their negatives (ties to the even code; sign bit, 2 exponent bits, 1
  *   mantissa bit).  No value saturates: the error is at most half a step.
  * A block with a value that is not finite has no scale: all of it stands for NaN.
- * The value of a code is code * s.
+ * The value of a code is code * s.  Magnitudes of 1.75 * 2^127 and more become 2^128,
+ * which fp32 and bf16 do not have: it reads back as infinite, and gradients that it has a
+ * part in are infinite or NaN; products take it as it is.
  * ------------------------------------------------------------------------- */
 
 /* A matrix of values: row r starts at data + r * stride elements, its columns lie
@@ -640,7 +642,7 @@ size_t octree_nca_mx4_code_bytes(int64_t rows, int64_t cols);
  * Errors: EINVAL, ESHAPE, EHIP. */
 int octree_nca_mx4_quantise(const octnca_rows *x, const octnca_mx4 *m, void *stream);
 
-/* x = the values of m, rounded once to x's type (fp16 past its range: infinite). */
+/* x = the values of m, rounded once to x's type (past its range: infinite). */
 int octree_nca_mx4_dequantise(const octnca_mx4 *m, const octnca_rows *x, void *stream);
 
 /* out[r][n] = sum over k of a[r][k] w[n][k] + bias[n], summed in fp32 and rounded
@@ -673,8 +675,8 @@ size_t octree_nca_mx4_backward_workspace_bytes(int64_t rows, int64_t cols, int64
  *   workspace    16-byte aligned; NULL is allowed without grad_weight and grad_bias.
  * Written arrays lie outside each other and outside what is read, and are
  * overwritten (rows = 0: with zeros).  The products take every bit of G (as sums of
- * bf16 values; what of them, of a and of w lies below 2^-126 may be lost), are summed in fp32 and in
- * an order that depends on the sizes only.
+ * bf16 values; what of them, of a and of w lies below 2^-126 may be lost, and 2^128 in a
+ * or w is infinite, times 0 NaN), are summed in fp32 and in an order that depends on the sizes only.
  * Errors: EINVAL, ESHAPE, ESPACE, EHIP. */
 int octree_nca_mx4_backward(const octnca_rows *grad_out, const octnca_mx4 *a, const octnca_mx4 *w,
                             const octnca_rows *grad_in, float *grad_weight, float *grad_bias,
