@@ -687,11 +687,15 @@ int octree_nca_mx4_backward(const octnca_rows *grad_out, const octnca_mx4 *a, co
  * (e >> 2, c), each as two words, lower first, and key seed, c = index + *step
  * (modulo 2^64); it is dropped iff the draw < T = min(2^32, floor(rate * 2^32)).
  * Another generator than the fire mask's: its draws cost half the multiplications,
- * and an element takes one where a cell takes one for all its channels. */
+ * and an element takes one where a cell takes one for all its channels.
+ * One seed and one c give one mask, whoever asks for it: with step counting on the
+ * device, a layer of index 1 would drop at step t what a layer of index 0 and the same
+ * seed drops at t + 1.  Layers take seeds of their own, or indices further apart than
+ * there are steps. */
 typedef struct {
     float rate;          /* in [0, 1] */
     uint64_t seed;
-    uint64_t index;      /* of the mask: a layer's number, a step, .. */
+    uint64_t index;      /* of the mask among the seed's */
     const int64_t *step; /* device [1], read by the kernel (a captured graph draws a new mask
                             each time it is replayed, if it counts), or NULL for 0 */
 } octnca_dropout;

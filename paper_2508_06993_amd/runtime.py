@@ -406,6 +406,8 @@ class CellLayer:
 class Dropout:
     """Dropout with a mask that is drawn anew in every call (octnca_dropout).
 
+    A mask is that of ``seed`` and index + step: each layer takes a seed of its own (of
+    one seed, index 1 drops at a step what index 0 drops at the next).
     ``step``: device int64 [1] that counts training steps, read by the kernel and
     added to ``index``, so that a captured graph draws a new mask each time it is
     replayed; the gradient has to see the same value as the forward."""
