@@ -455,14 +455,24 @@ hipError_t run_few(const ProductArgs &p, const octnca_rows *x, int cols, hipStre
                     (unsigned)((p.a.rows + kMxGroup * G - 1) / (kMxGroup * G)));
     const void *from = x ? x->data : nullptr;
     const int64_t stride = x ? x->stride : 0;
-    // Sixteen waves where there are few workgroups, two where there are few columns to
-    // split: 1000 x 517 -> 1003 takes 9.5 us with four, 7.8 with two, 9.5 with one.
-    if ((int64_t)grid.x * grid.y <= 128 && p.a.blocks > 16)
+    constexpr bool kValues = !std::is_same<X, int>::value;
+    // Sixteen waves where a workgroup has much to read or to quantise and there are no
+    // more workgroups than compute units, two where codes have few columns to split.  us
+    // with sixteen, four and two.  Codes, -> 1024: 1 x 4096 3.5, 3.1, 3.5, 1 x 8192 3.5,
+    // 4.1, 4.9; 64 x 8192 8.8, 7.8, 10.3, 64 x 32768 22.3, 24.4, 33.8; 1000 x 517 -> 1003
+    // 20.2, 7.7, 6.7, 1 x 1100 3.1, 2.5, 2.8.  Values: 1 x 4096 -> 1024 3.8, 3.9, 5.2, 16 x
+    // 1024 -> 4096 5.2, 6.4, 9.8 and -> 16384 (1024 workgroups) 14.0, 10.0, 10.5.
+    if ((int64_t)grid.x * grid.y <= 256 &&
+        (kValues ? p.a.rows * p.a.blocks > 128 : p.a.blocks >= (G == 4 ? 512 : 192))) {
         few_rows<V, X, G, 16><<<grid, 64 * 16, 0, stream>>>(p, from, stride, cols);
-    else if (p.a.blocks <= 32)
-        few_rows<V, X, G, 2><<<grid, 64 * 2, 0, stream>>>(p, from, stride, cols);
-    else
-        few_rows<V, X, G, 4><<<grid, 64 * 4, 0, stream>>>(p, from, stride, cols);
+        return hipGetLastError();
+    }
+    if constexpr (!kValues)
+        if (p.a.blocks <= 32) {
+            few_rows<V, X, G, 2><<<grid, 64 * 2, 0, stream>>>(p, from, stride, cols);
+            return hipGetLastError();
+        }
+    few_rows<V, X, G, 4><<<grid, 64 * 4, 0, stream>>>(p, from, stride, cols);
     return hipGetLastError();
 }
 

@@ -37,7 +37,10 @@ PRODUCTS = [  # rows, cols, outs
     (33, 128, 129), (40, 1000, 300), (50, 1100, 4099), (64, 33, 2), (100, 300, 70),
     (300, 1024, 520), (300, 20000, 300), (1000, 16, 19), (1000, 517, 1003), (1031, 20, 100),
     (5000, 32, 64), (20011, 64, 16), (4099, 100, 20), (3001, 128, 128), (1100, 2080, 1050),
-    (4096, 4096, 512), (4100, 610, 4100), (900_001, 32, 64)]
+    (4096, 4096, 512), (4100, 610, 4100), (900_001, 32, 64),
+    # each number of waves, for each number of rows that they take
+    (16, 1024, 4096), (4, 1030, 1000), (16, 1024, 4100), (1, 8200, 2000), (20, 6200, 1000),
+    (20, 4100, 1000), (30, 1000, 1003), (40, 16400, 300), (64, 16300, 300), (1, 300, 4099)]
 
 
 @pytest.mark.parametrize("rows,cols,outs", PRODUCTS)
