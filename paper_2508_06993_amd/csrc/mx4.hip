@@ -443,10 +443,12 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
     });
 }
 
-// Which kernel serves a product that is not narrow: large tiles, tiles of 128 x 128
-// where there are 128 of them, else a few rows at a time with the columns split.  us of
-// tiles and of few rows, 4096 -> 4096: 512 rows (128 tiles) 24 and 22, 768 rows 25 and
-// 30, 1024 rows 26 and 39.
+// Which kernel serves a product that is not narrow: large tiles, tiles of 128 x 128 for
+// more than 64 rows where there are 128 of them (160, if rows have more than 48 blocks), else
+// a few rows at a time with the columns split.  us of tiles and of few rows: 512 x 300 ->
+// 4096 (128 tiles) 8.4 and 9.9, 384 x 300 (96) 8.1 and 7.3; 512 x 4096 -> 4096 24.1 and
+// 20.7, 640 x 4096 (160) 24.5 and 24.9, 768 x 4096 24.9 and 28.2; 65 x 4096 -> 16384 24.2 and
+// 20.0, 64 rows 23.9 and 13.2, 64 x 4096 -> 32768 (256) 25.9 and 21.9.
 namespace {
 
 template <typename V, typename X, int G>
@@ -494,7 +496,7 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
                 p, (int)large.first, (int)large.second);
             return hipGetLastError();
         }
-        if (a.rows > 64 && small.first * small.second >= 128) {
+        if (a.rows > 64 && small.first * small.second >= (p.a.blocks > 48 ? 160 : 128)) {
             product_tiles<V, 4, 2><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
                 p, (int)small.first, (int)small.second);
             return hipGetLastError();

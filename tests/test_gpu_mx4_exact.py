@@ -40,7 +40,9 @@ PRODUCTS = [  # rows, cols, outs
     (4096, 4096, 512), (4100, 610, 4100), (900_001, 32, 64),
     # each number of waves, for each number of rows that they take
     (16, 1024, 4096), (4, 1030, 1000), (16, 1024, 4100), (1, 8200, 2000), (20, 6200, 1000),
-    (20, 4100, 1000), (30, 1000, 1003), (40, 16400, 300), (64, 16300, 300), (1, 300, 4099)]
+    (20, 4100, 1000), (30, 1000, 1003), (40, 16400, 300), (64, 16300, 300), (1, 300, 4099),
+    # both sides of the number of tiles from which they are taken
+    (512, 1530, 4096), (512, 1540, 4096), (640, 1540, 4096), (1020, 300, 1920), (65, 300, 16384)]
 
 
 @pytest.mark.parametrize("rows,cols,outs", PRODUCTS)
