@@ -609,10 +609,12 @@ template <typename V, bool WEIGHT>
 void run(const BackwardArgs &b, int splits, bool products, hipStream_t stream) {
     if (mx4_large_tiles(WEIGHT ? b.outs : b.rows, b.cols))
         return run_tiles<V, WEIGHT, kLarge>(b, splits, products, stream);
-    // more workgroups of a quarter of the tile: 1000 x 517 <- 1003 in bf16 35 us of all
-    // three gradients, with tiles of 128 x 128 43
+    // More workgroups of a quarter of the tile, for up to 128 tiles.  us of grad_in with them
+    // and with tiles of 128 x 128, bf16: 40 tiles (1000 x 517 <- 1003) 12.5 and 20.4, 64 (1000
+    // x 1024 <- 1024) 10.3 and 16.6, 128 (2048 x 1024 <- 1024) 13.9 and 16.6, 192 (2048 x 1500
+    // <- 1000) 18.6 and 17.7; fp32, of the last two, 33 and 41, 43.5 and 42.9.
     if constexpr (!WEIGHT)
-        if (((b.rows + 127) / 128) * ((b.cols + 127) / 128) < 64)
+        if (((b.rows + 127) / 128) * ((b.cols + 127) / 128) <= 128)
             return run_tiles<V, WEIGHT, kTiny>(b, splits, products, stream);
     run_tiles<V, WEIGHT, kSmall>(b, splits, products, stream);
 }

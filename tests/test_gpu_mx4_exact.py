@@ -70,7 +70,9 @@ GRADIENTS = [  # rows, cols, outs
     (1031, 20, 100), (5003, 32, 64), (102_401, 32, 64), (20011, 64, 16), (2000, 128, 60),
     (2000, 60, 128), (999, 128, 128), (40000, 40, 3), (100_003, 100, 30), (700, 640, 600),
     (130, 1100, 257), (1000, 517, 1003), (13001, 1030, 133), (100_000, 300, 40),
-    (300, 3500, 3700), (500, 3584, 3600), (6000, 4096, 4100)]
+    (300, 3500, 3700), (500, 3584, 3600), (6000, 4096, 4100),
+    # both sides of the number of tiles up to which grad_in takes small ones
+    (1000, 1024, 1024), (2030, 1000, 500), (2060, 1000, 131)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
