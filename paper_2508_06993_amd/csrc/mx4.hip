@@ -216,8 +216,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows(ProductArgs p, const void
 
 // Tile of a workgroup among row_tiles x col_tiles.  Workgroups go round the eight dies,
 // each with its own L2: a die takes tiles in a row, which run down eight row tiles
-// before they go to the next columns.  us with this and with tiles in plain order, 4096
-// -> 4096: 512 rows 24 and 26, 1024 rows 26 and 27; large tiles: no difference.
+// before they go to the next columns.  us with this and with tiles in plain order, 1024 x
+// 4096 -> 4096: 26 and 27; large tiles: no difference.
 struct Tile {
     int row, col;
 };
@@ -230,11 +230,11 @@ __device__ __forceinline__ Tile die_tile(int id, int row_tiles, int col_tiles) {
 }
 
 // Large products.  A workgroup takes 32 S rows times 32 S outputs, a wave a quarter of
-// them with its sums in registers.  128 columns at a time (four blocks) go through
-// LDS, loaded two steps ahead of their use: one step's products take about half of
-// the time that a load takes to come back.  Blocks past the last come as codes 0 with
-// scale 1.  The weights' rows go to the operands so that a lane ends up with 16 bytes of
-// outputs in a row, and the four lanes of a row with 64.
+// them with its sums in registers.  A step takes 4 U blocks (256 columns) through LDS: the
+// next one's are loaded during the first half of its products and go to the other half of
+// LDS during the second.  Blocks past the last come as codes 0 with scale 1.  The weights'
+// rows go to the operands so that a lane ends up with 16 bytes of outputs in a row, and the
+// two lanes of a row with 32.
 template <typename V, int S, int U>
 __global__ __launch_bounds__(kThreads) void product_tiles(ProductArgs p, int row_tiles,
                                                           int out_tiles) {

@@ -215,8 +215,8 @@ template <typename V, int KB, int NT>
 hipError_t run(const NarrowArgs &b, hipStream_t stream) {
     const int64_t per = KB == 4 ? b.a.blocks : 4;
     const int64_t turns = (b.units + per - 1) / per;
-    // as many workgroups as are resident; us of the two cases above with 2, 3, 4 and 8 a
-    // compute unit: 63, 63, 70, 70 and 38, 29, 27, 29
+    // as many workgroups as are resident; us with 2, 3, 4 and 8 a compute unit: 1M x 32
+    // fp32 values -> 64 fp16 63, 63, 70, 70, 1M x 64 codes -> 19 fp32 38, 29, 27, 29
     const int64_t grid = std::min<int64_t>((turns + kWaves - 1) / kWaves,
                                            (std::is_same<V, int>::value ? 4 : 3) * device_cus());
     narrow<V, KB, NT><<<(unsigned)grid, kThreads, 0, stream>>>(b);
