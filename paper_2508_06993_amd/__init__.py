@@ -863,11 +863,10 @@ def _on_device(t, name):
 def _here(*matrices):
     """Refuses matrices in 4 bits whose memory the current device's kernels would not be
     given."""
-    device = _current_device()
     for m in matrices:
-        if m.device is not None and m.device != device:
+        if m.device is not None and m.device != _current_device():
             raise OctreeNCAError(f"matrix in 4 bits: on cuda:{m.device}, the current device is "
-                                 f"{device}")
+                                 f"{_current_device()}")
 
 
 def _rows(t, name, rows=None, cols=None):

@@ -54,3 +54,10 @@ def test_a_struct_remembers_its_device(monkeypatch):
     monkeypatch.setattr(octnca, "_ptr", lambda t, dtype, name: 0x1000)
     m = octnca.MX4Buffers(3, 40, *(Codes(s) for s in octnca.mx4_shapes(3, 40))).struct()
     assert m.device == 1
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_host_tensors_without_asking_for_a_device(library_path, monkeypatch, call):
+    monkeypatch.setattr(octnca, "_current_device", None)
+    with pytest.raises(octnca.OctreeNCAError, match="must be a device"):
+        CALLS[call](here())
