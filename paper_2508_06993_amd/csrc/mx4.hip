@@ -443,13 +443,19 @@ hipError_t launch_mx4_dequantise(const octnca_mx4 &m, const octnca_rows &x, hipS
     });
 }
 
-// Which kernel serves a product that is not narrow: large tiles, tiles of 128 x 128 for
-// more than 64 rows where there are 128 of them (160, if rows have more than 48 blocks), else
-// a few rows at a time with the columns split.  us of tiles and of few rows: 512 x 300 ->
-// 4096 (128 tiles) 8.4 and 9.9, 384 x 300 (96) 8.1 and 7.3; 512 x 4096 -> 4096 24.1 and
-// 20.7, 640 x 4096 (160) 24.5 and 24.9, 768 x 4096 24.9 and 28.2; 65 x 4096 -> 16384 24.2 and
-// 20.0, 64 rows 23.9 and 13.2, 64 x 4096 -> 32768 (256) 25.9 and 21.9.
 namespace {
+
+// Which kernel serves a product that is not narrow: large tiles; for more than 64 rows 128 of
+// the tiles of 128 x 128 and more (160 for up to 1024 rows of more than 48 blocks); else a
+// few rows at a time with the columns split, where each die reads all rows for itself.  us of
+// tiles and of few rows: 512 x 300 -> 4096 (128 tiles) 8.4 and 9.9, 384 x 300 (96) 8.1 and
+// 7.3; 512 x 4096 -> 4096 24.1 and 20.7, 640 x 4096 (160) 24.5 and 24.9, 768 x 4096 24.9 and
+// 28.2; 16384 x 4096 -> 128 (128) 24.8 and 43.6, 10300 -> 128 (81) 23.9 and 30.0, 8000 -> 128 (63)
+// 23.7 and 23.1, 12000 -> 16 (94) 22 and 8; 65 x 4096 -> 16384 24.2 and 20.0, 64 rows 23.9 and
+// 13.2, 64 x 4096 -> 32768 (256) 25.9 and 21.9.
+bool takes_tiles(int64_t rows, int blocks, int64_t tiles) {
+    return rows > 64 && tiles >= (rows <= 1024 && blocks > 48 ? 160 : 128);
+}
 
 template <typename V, typename X, int G>
 hipError_t run_few(const ProductArgs &p, const octnca_rows *x, int cols, hipStream_t stream) {
@@ -459,22 +465,19 @@ hipError_t run_few(const ProductArgs &p, const octnca_rows *x, int cols, hipStre
     const int64_t stride = x ? x->stride : 0;
     constexpr bool kValues = !std::is_same<X, int>::value;
     // Sixteen waves where a workgroup has much to read or to quantise and there are no
-    // more workgroups than compute units, two where codes have few columns to split.  us
-    // with sixteen, four and two.  Codes, -> 1024: 1 x 4096 3.5, 3.1, 3.5, 1 x 8192 3.5,
-    // 4.1, 4.9; 64 x 8192 8.8, 7.8, 10.3, 64 x 32768 22.3, 24.4, 33.8; 1000 x 517 -> 1003
-    // 20.2, 7.7, 6.7, 1 x 1100 3.1, 2.5, 2.8.  Values: 1 x 4096 -> 1024 3.8, 3.9, 5.2, 16 x
-    // 1024 -> 4096 5.2, 6.4, 9.8 and -> 16384 (1024 workgroups) 14.0, 10.0, 10.5.
-    if ((int64_t)grid.x * grid.y <= 256 &&
-        (kValues ? p.a.rows * p.a.blocks > 128 : p.a.blocks >= (G == 4 ? 512 : 192))) {
+    // more workgroups than compute units, two where it has little.  us with sixteen, four
+    // and two.  Codes, -> 1024: 1 x 4096 3.5, 3.1, 3.5, 1 x 8192 3.5, 4.1, 4.9; 64 x 8192 8.8,
+    // 7.8, 10.3, 64 x 32768 22.3, 24.4, 33.8; 1000 x 517 -> 1003 20.2, 7.7, 6.7, 1 x 1100 3.1,
+    // 2.5, 2.8.  Values: 1 x 1024 -> 300 3.3, 3.1, 3.0, 1 x 2048 -> 1024 3.6, 3.2, 3.7, 1 x 4096
+    // 3.8, 3.9, 5.2, 16 x 1024 -> 4096 5.2, 6.4, 9.8 and -> 16384 (1024 workgroups) 14.0, 10.0,
+    // 10.5.
+    const int64_t work = kValues ? p.a.rows * p.a.blocks : p.a.blocks;
+    if ((int64_t)grid.x * grid.y <= 256 && work >= (kValues ? 80 : G == 4 ? 512 : 192))
         few_rows<V, X, G, 16><<<grid, 64 * 16, 0, stream>>>(p, from, stride, cols);
-        return hipGetLastError();
-    }
-    if constexpr (!kValues)
-        if (p.a.blocks <= 32) {
-            few_rows<V, X, G, 2><<<grid, 64 * 2, 0, stream>>>(p, from, stride, cols);
-            return hipGetLastError();
-        }
-    few_rows<V, X, G, 4><<<grid, 64 * 4, 0, stream>>>(p, from, stride, cols);
+    else if (work <= 32)
+        few_rows<V, X, G, 2><<<grid, 64 * 2, 0, stream>>>(p, from, stride, cols);
+    else
+        few_rows<V, X, G, 4><<<grid, 64 * 4, 0, stream>>>(p, from, stride, cols);
     return hipGetLastError();
 }
 
@@ -496,7 +499,7 @@ hipError_t launch_mx4_product(const octnca_mx4 &a, const octnca_mx4 &w, const fl
                 p, (int)large.first, (int)large.second);
             return hipGetLastError();
         }
-        if (a.rows > 64 && small.first * small.second >= (p.a.blocks > 48 ? 160 : 128)) {
+        if (takes_tiles(a.rows, p.a.blocks, small.first * small.second)) {
             product_tiles<V, 4, 2><<<(unsigned)(small.first * small.second), kThreads, 0, stream>>>(
                 p, (int)small.first, (int)small.second);
             return hipGetLastError();

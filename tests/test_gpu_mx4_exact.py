@@ -42,7 +42,8 @@ PRODUCTS = [  # rows, cols, outs
     (16, 1024, 4096), (4, 1030, 1000), (16, 1024, 4100), (1, 8200, 2000), (20, 6200, 1000),
     (20, 4100, 1000), (30, 1000, 1003), (40, 16400, 300), (64, 16300, 300), (1, 300, 4099),
     # both sides of the number of tiles from which they are taken
-    (512, 1530, 4096), (512, 1540, 4096), (640, 1540, 4096), (1020, 300, 1920), (65, 300, 16384)]
+    (512, 1530, 4096), (512, 1540, 4096), (640, 1540, 4096), (1020, 300, 1920), (65, 300, 16384),
+    (1030, 1540, 1920), (10300, 1540, 3), (16300, 1540, 100)]
 
 
 @pytest.mark.parametrize("rows,cols,outs", PRODUCTS)
